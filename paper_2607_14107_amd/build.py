@@ -22,7 +22,8 @@ LIB = os.path.join(PKG, "libpolestar.so")
 ARCH = "gfx950"
 
 SOURCES = ["api.hip", "drift.hip", "select.hip", "gemm.hip", "gemm_tile.hip", "gemm_qkv.hip", "attend.hip",
-           "attend_ring.hip", "commit.hip", "step.hip", "proxy.hip", "model.hip", "codec.hip"]
+           "attend_ring.hip", "commit.hip", "step.hip", "proxy.hip", "model.hip", "codec.hip",
+           "mx_quant.hip", "mx_gemm.hip", "mx_attend.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -146,6 +146,26 @@ def lib() -> ctypes.CDLL:
     L.polestar_residual_add.argtypes = [I, Lg, P, P, P]
     L.polestar_copy_rows.restype = S
     L.polestar_copy_rows.argtypes = [I, I, I, I, P, P, P, P, I, I, I, P]
+    L.polestar_mx_quantize.restype = S
+    L.polestar_mx_quantize.argtypes = [I, I, I, I, I, I, I, P, P, P, P]
+    L.polestar_mx_dequantize.restype = S
+    L.polestar_mx_dequantize.argtypes = [I, I, Lg, I, P, P, P, P]
+    L.polestar_mx_linear_workspace_size.restype = Z
+    L.polestar_mx_linear_workspace_size.argtypes = [I, I, Lg, I, I]
+    L.polestar_mx_linear.restype = S
+    L.polestar_mx_linear.argtypes = [I, I, Lg, I, I, P, P, P, P, P, P, Z, P]
+    L.polestar_mx_quantize_linear_workspace_size.restype = Z
+    L.polestar_mx_quantize_linear_workspace_size.argtypes = [I, I, I, I, I, I]
+    L.polestar_mx_quantize_linear.restype = S
+    L.polestar_mx_quantize_linear.argtypes = [I, I, I, I, I, I, I, I, P, P, P, P, P, Z, P]
+    L.polestar_residual_rmsnorm_mx.restype = S
+    L.polestar_residual_rmsnorm_mx.argtypes = [I, I, Lg, I, P, P, P, F, P, P, P, P]
+    L.polestar_mx_store_kv.restype = S
+    L.polestar_mx_store_kv.argtypes = [I, I, I, I, I, I, P, P, Lg, P, P, I, P, P, P, P, P]
+    L.polestar_mx_attend_workspace_size.restype = Z
+    L.polestar_mx_attend_workspace_size.argtypes = [I, I, I, I, I, I, I]
+    L.polestar_mx_attend.restype = S
+    L.polestar_mx_attend.argtypes = [I, I, I, I, I, I, I, P, Lg, P, P, P, P, P, F, P, P, P, Z, P]
     _lib = L
     return L
 
@@ -573,6 +593,224 @@ def codec_gather(fmt: int, codes: torch.Tensor, scales: torch.Tensor, idx: torch
         fmt, dt, b, seq, d, _ptr(codes, torch.uint8), _ptr(scales, torch.uint8), _ptr(idx, torch.int32),
         _ptr(count, torch.int32), k_max, _ptr(labels, torch.int32), means.shape[1], _ptr(means, torch.float32),
         float(eps), _ptr(x_out, torch.float32), _ptr(h_out), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# a layer's forward in the microscaling formats (include/polestar_mx.h)
+# ---------------------------------------------------------------------------
+
+def _mx_device(*tensors) -> torch.device:
+    """The one device of the given tensors, which has to be the current one."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("tensor must be on the GPU")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("tensors are on different devices")
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+    return dev
+
+
+def _mx_empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A new tensor for work on `stream`: kept from reuse until that is done where it is not the current stream."""
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None and stream != torch.cuda.current_stream():
+        t.record_stream(stream)
+    return t
+
+
+def _mx_workspace(nbytes: int, device, ws: torch.Tensor | None, stream):
+    if nbytes == 0 or (ws is not None and ws.numel() * ws.element_size() >= nbytes):
+        return ws
+    return _mx_empty(nbytes, torch.uint8, device, stream)
+
+
+def _mx_codes(fmt: int, codes: torch.Tensor, scales: torch.Tensor, what: str) -> int:
+    """Channels of a row held in codes [..., row bytes] and scales [..., n / 32]."""
+    n = 32 * scales.shape[-1]
+    if codes.shape[-1] != (n // 2 if fmt == MXFP4 else n) or codes.shape[:-1] != scales.shape[:-1]:
+        raise ValueError(f"{what}: codes and scales do not match")
+    return n
+
+
+def _mx_row_stride(t: torch.Tensor, what: str) -> int:
+    """Elements from row to row of t [batch][rows][heads][head_dim], whose heads lie one after another."""
+    b, n, heads, hd = t.shape
+    s = t.stride()
+    if t.numel() == 0:
+        return heads * hd
+    rs = s[1] if n > 1 else (s[0] if b > 1 else heads * hd)
+    if (s[3] != 1 and hd > 1) or (s[2] != hd and heads > 1) or (b > 1 and s[0] != n * rs):
+        raise ValueError(f"{what}: rows must be equally spaced and whole")
+    return rs
+
+
+def mx_quantize(fmt: int, x: torch.Tensor, row_start: int = 0, n_rows: int | None = None,
+                codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, stream=None):
+    """Rows [row_start, row_start + n_rows) of x [batch][seq][n] (or all of a [rows][n] matrix) as
+    (codes, scales) in MXFP4 or MXFP8, shaped like the rows."""
+    if x.dim() == 2:
+        lead, (b, seq) = (x.shape[0],), (1, x.shape[0])
+        if row_start != 0 or n_rows not in (None, seq):
+            raise ValueError("mx_quantize: a matrix is taken whole")
+        n_rows = seq
+    else:
+        b, seq, _ = x.shape
+        n_rows = seq - row_start if n_rows is None else n_rows
+        lead = (b, n_rows)
+    n = x.shape[-1]
+    dev = _mx_device(x, codes, scales)
+    if codes is None:
+        codes = _mx_empty((*lead, n // 2 if fmt == MXFP4 else n), torch.uint8, dev, stream)
+    if scales is None:
+        scales = _mx_empty((*lead, n // 32), torch.uint8, dev, stream)
+    if _mx_codes(fmt, codes, scales, "mx_quantize") != n or scales.numel() * 32 != b * n_rows * n:
+        raise ValueError("mx_quantize: shapes do not match")
+    _check("polestar_mx_quantize", lib().polestar_mx_quantize(
+        fmt, _dtype_code(x), b, seq, n, row_start, n_rows, _ptr(x), _ptr(codes, torch.uint8),
+        _ptr(scales, torch.uint8), _stream(stream)))
+    return codes, scales
+
+
+def mx_dequantize(fmt: int, codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None) -> torch.Tensor:
+    """The values of codes [..., row bytes] and scales [..., n / 32] into out [..., n] (float32 or bfloat16)."""
+    n = _mx_codes(fmt, codes, scales, "mx_dequantize")
+    if tuple(out.shape) != (*codes.shape[:-1], n):
+        raise ValueError("mx_dequantize: shapes do not match")
+    _mx_device(codes, scales, out)
+    _check("polestar_mx_dequantize", lib().polestar_mx_dequantize(
+        fmt, _dtype_code(out), out.numel() // n if n else 0, n, _ptr(codes, torch.uint8), _ptr(scales, torch.uint8),
+        _ptr(out), _stream(stream)))
+    return out
+
+
+def mx_linear_workspace_size(x_fmt: int, dtype: int, rows: int, n_out: int, n_in: int) -> int:
+    return lib().polestar_mx_linear_workspace_size(x_fmt, dtype, rows, n_out, n_in)
+
+
+def mx_linear(x_fmt: int, x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor,
+              w_scales: torch.Tensor, y: torch.Tensor, workspace: torch.Tensor | None = None,
+              stream=None) -> torch.Tensor:
+    """y[..., o] = sum_i x[..., i] w[o, i]: rows in MXFP8 or MXFP4, weights in MXFP4, y float32 or bfloat16."""
+    n_in = _mx_codes(x_fmt, x_codes, x_scales, "mx_linear")
+    n_out = w_codes.shape[0]
+    if (_mx_codes(MXFP4, w_codes, w_scales, "mx_linear") != n_in or w_codes.dim() != 2
+            or tuple(y.shape) != (*x_codes.shape[:-1], n_out)):
+        raise ValueError("mx_linear: shapes do not match")
+    dev = _mx_device(x_codes, x_scales, w_codes, w_scales, y, workspace)
+    rows, dt = y.numel() // n_out, _dtype_code(y)
+    ws = _mx_workspace(mx_linear_workspace_size(x_fmt, dt, rows, n_out, n_in), dev, workspace, stream)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check("polestar_mx_linear", lib().polestar_mx_linear(
+        x_fmt, dt, rows, n_in, n_out, _ptr(x_codes, torch.uint8), _ptr(x_scales, torch.uint8),
+        _ptr(w_codes, torch.uint8), _ptr(w_scales, torch.uint8), _ptr(y), _ptr(ws), nbytes, _stream(stream)))
+    return y
+
+
+def mx_quantize_linear_workspace_size(x_fmt: int, dtype: int, batch: int, n_rows: int, n_out: int, n_in: int) -> int:
+    return lib().polestar_mx_quantize_linear_workspace_size(x_fmt, dtype, batch, n_rows, n_out, n_in)
+
+
+def mx_quantize_linear(x_fmt: int, x: torch.Tensor, row_start: int, n_rows: int, w_codes: torch.Tensor,
+                       w_scales: torch.Tensor, y: torch.Tensor, workspace: torch.Tensor | None = None,
+                       stream=None) -> torch.Tensor:
+    """mx_quantize of rows [row_start, row_start + n_rows) of x [batch][seq][n_in], then mx_linear of them into
+    y [batch][n_rows][n_out] (x's dtype)."""
+    b, seq, n_in = x.shape
+    n_out = w_codes.shape[0]
+    if (_mx_codes(MXFP4, w_codes, w_scales, "mx_quantize_linear") != n_in or w_codes.dim() != 2
+            or tuple(y.shape) != (b, n_rows, n_out)):
+        raise ValueError("mx_quantize_linear: shapes do not match")
+    dev = _mx_device(x, w_codes, w_scales, y, workspace)
+    dt = _dtype_code(x)
+    ws = _mx_workspace(mx_quantize_linear_workspace_size(x_fmt, dt, b, n_rows, n_out, n_in), dev, workspace, stream)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check("polestar_mx_quantize_linear", lib().polestar_mx_quantize_linear(
+        x_fmt, dt, b, seq, n_in, n_out, row_start, n_rows, _ptr(x), _ptr(w_codes, torch.uint8),
+        _ptr(w_scales, torch.uint8), _ptr(y, x.dtype), _ptr(ws), nbytes, _stream(stream)))
+    return y
+
+
+def residual_rmsnorm_mx(fmt: int, x: torch.Tensor, y: torch.Tensor | None, x_out: torch.Tensor | None,
+                        codes: torch.Tensor, scales: torch.Tensor, gain: torch.Tensor | None = None,
+                        eps: float = 1e-5, stream=None) -> None:
+    """x_out = x + y (float32; x_out may be x, y may be None), then codes and scales of RMSNorm(x_out) * gain.
+    x [..., d], codes [..., row bytes], scales [..., d / 32]."""
+    d = x.shape[-1]
+    if (_mx_codes(fmt, codes, scales, "residual_rmsnorm_mx") != d or codes.shape[:-1] != x.shape[:-1]
+            or (y is not None and (y.shape != x.shape or x_out is None))
+            or (x_out is not None and x_out.shape != x.shape) or (gain is not None and tuple(gain.shape) != (d,))):
+        raise ValueError("residual_rmsnorm_mx: shapes do not match")
+    _mx_device(x, y, x_out, codes, scales, gain)
+    _check("polestar_residual_rmsnorm_mx", lib().polestar_residual_rmsnorm_mx(
+        fmt, BF16 if y is None else _dtype_code(y), x.numel() // d, d, _ptr(x, torch.float32), _ptr(y),
+        _ptr(gain, torch.float32), float(eps), _ptr(x_out, torch.float32), _ptr(codes, torch.uint8),
+        _ptr(scales, torch.uint8), _stream(stream)))
+
+
+def _mx_caches(k_codes, k_scales, v_codes, v_scales, what: str):
+    """(batch, n_kv_heads, seq, head_dim) of K/V caches in MXFP4."""
+    b, kvh, seq, _ = k_codes.shape
+    hd = _mx_codes(MXFP4, k_codes, k_scales, what)
+    if _mx_codes(MXFP4, v_codes, v_scales, what) != hd or v_codes.shape != k_codes.shape:
+        raise ValueError(f"{what}: the caches differ in shape")
+    return b, kvh, seq, hd
+
+
+def mx_store_kv(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor,
+                v_codes: torch.Tensor, v_scales: torch.Tensor, row_start: int = 0, idx: torch.Tensor | None = None,
+                count: torch.Tensor | None = None, stream=None) -> None:
+    """Quantize the rows k, v [batch][n_rows][n_kv_heads][head_dim] (equally spaced rows, e.g. cut from a joint
+    product) into caches [batch][n_kv_heads][seq][...], at the positions idx[b][0 .. count[b]) or from row_start on."""
+    b, kvh, seq, hd = _mx_caches(k_codes, k_scales, v_codes, v_scales, "mx_store_kv")
+    n = k.shape[1]
+    if tuple(k.shape) != (b, n, kvh, hd) or v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("mx_store_kv: shapes or dtypes do not match")
+    if (idx is not None and tuple(idx.shape) != (b, n)) or (count is not None and (idx is None or tuple(count.shape) != (b,))):
+        raise ValueError("mx_store_kv: idx must be [batch][n_rows], count [batch] and given with idx")
+    rs = _mx_row_stride(k, "mx_store_kv")
+    if n > 0 and _mx_row_stride(v, "mx_store_kv") != rs and n * b > 1:
+        raise ValueError("mx_store_kv: k and v differ in row stride")
+    _mx_device(k, v, k_codes, k_scales, v_codes, v_scales, idx, count)
+    _check("polestar_mx_store_kv", lib().polestar_mx_store_kv(
+        _dtype_code(k), b, seq, kvh, hd, n, k.data_ptr(), v.data_ptr(), rs, _ptr(idx, torch.int32),
+        _ptr(count, torch.int32), row_start, _ptr(k_codes, torch.uint8), _ptr(k_scales, torch.uint8),
+        _ptr(v_codes, torch.uint8), _ptr(v_scales, torch.uint8), _stream(stream)))
+
+
+def mx_attend_workspace_size(dtype: int, batch: int, seq: int, n_heads: int, n_kv_heads: int, head_dim: int,
+                             n_rows: int) -> int:
+    return lib().polestar_mx_attend_workspace_size(dtype, batch, seq, n_heads, n_kv_heads, head_dim, n_rows)
+
+
+def mx_attend(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor, v_codes: torch.Tensor,
+              v_scales: torch.Tensor, kv_len: torch.Tensor | None = None, out: torch.Tensor | None = None,
+              lse: torch.Tensor | None = None, scale: float = 0.0, workspace: torch.Tensor | None = None,
+              stream=None) -> torch.Tensor:
+    """Attention of q [batch][n_rows][n_heads][head_dim] (equally spaced rows) over the first kv_len[b] positions
+    (all without kv_len) of K/V caches in MXFP4 [batch][n_kv_heads][seq][...] -> out, q's shape."""
+    b, kvh, seq, hd = _mx_caches(k_codes, k_scales, v_codes, v_scales, "mx_attend")
+    n, heads = q.shape[1], q.shape[2]
+    if (tuple(q.shape) != (b, n, heads, hd) or (kv_len is not None and tuple(kv_len.shape) != (b,))
+            or (out is not None and out.shape != q.shape) or (lse is not None and tuple(lse.shape) != (b, heads, n))):
+        raise ValueError("mx_attend: shapes do not match")
+    dev = _mx_device(q, k_codes, k_scales, v_codes, v_scales, kv_len, out, lse, workspace)
+    dt = _dtype_code(q)
+    if out is None:
+        out = _mx_empty(q.shape, q.dtype, dev, stream)
+    ws = _mx_workspace(mx_attend_workspace_size(dt, b, seq, heads, kvh, hd, n), dev, workspace, stream)
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check("polestar_mx_attend", lib().polestar_mx_attend(
+        dt, b, seq, heads, kvh, hd, n, q.data_ptr(), _mx_row_stride(q, "mx_attend"), _ptr(k_codes, torch.uint8),
+        _ptr(k_scales, torch.uint8), _ptr(v_codes, torch.uint8), _ptr(v_scales, torch.uint8),
+        _ptr(kv_len, torch.int32), float(scale), _ptr(out, q.dtype), _ptr(lse, torch.float32), _ptr(ws), nbytes,
+        _stream(stream)))
+    return out
 
 
 # ---------------------------------------------------------------------------
