@@ -12,6 +12,8 @@
 // 1.5e-5 of the result's norm on normal data, which fp32 would show.  With MXFP4
 // rows the products of a block span less than those bits and the sums are exact
 // to fp32.
+#include <type_traits>
+
 #include "host_common.hpp"
 #include "mx_dev.hpp"
 
@@ -21,16 +23,37 @@ namespace {
 struct MxGemmArgs {
     const uint8_t *x, *xs, *w, *ws;
     char* y;
+    float* part;                                         // split K: partials [split][rows][n_out]
     long rows;
     int n_out, n_in;
+    int ksplit, steps;                                   // K tiles of a split
+    int row_tiles, col_tiles;
 };
 
-// Operand fragments of a 64-channel step: lane l holds row l % 32, and of its
-// channels the block l / 32 (h).
+// A K tile is 128 channels: operand fragments of the 16x16x128 instruction, lane l
+// holding row l % 16 and the scale of block g = l / 16.  DEC: decoded to bf16 for
+// four 16x16x32 instructions.
+//
+// Rows in LDS: 16-byte chunks, XOR-swizzled so that the lanes whose reads run
+// together (0-3, 12-15, 20-27 of each 32, and the others) lie in different banks.
+// With rows of 64 bytes swizzled by row / 4 half the LDS cycles of an MXFP4 product
+// were conflicts; by its negative none are.
+template <int FMT> struct LdsRow;
+template <> struct LdsRow<POLESTAR_MXFP4> {
+    static constexpr int kBytes = 64;
+    __device__ __forceinline__ static int chunk(int row, int c) { return (c ^ (-(row >> 2) & 3)) << 4; }
+};
+template <> struct LdsRow<POLESTAR_MXFP8> {
+    static constexpr int kBytes = 128;
+    __device__ __forceinline__ static int chunk(int row, int c) { return (c ^ ((row >> 1) & 7)) << 4; }
+};
+
 template <int FMT, bool DEC> struct Frag;
 template <bool DEC> struct Frag<POLESTAR_MXFP4, DEC> {
-    uint4 c;
-    __device__ __forceinline__ void load(const uint8_t* row, int step, int h) { c = ld16(row + 32 * step + 16 * h); }
+    uint4 c;                                             // channels 32 g ..
+    __device__ __forceinline__ void load(const char* tile, int r, int g) {
+        c = ld16(tile + r * 64 + LdsRow<POLESTAR_MXFP4>::chunk(r, g));
+    }
     __device__ __forceinline__ intx8 codes() const {
         return intx8{static_cast<int>(c.x), static_cast<int>(c.y), static_cast<int>(c.z), static_cast<int>(c.w), 0, 0, 0, 0};
     }
@@ -39,14 +62,13 @@ template <bool DEC> struct Frag<POLESTAR_MXFP4, DEC> {
         o[2] = mx_fp4_bf16(c.z, sc); o[3] = mx_fp4_bf16(c.w, sc);
     }
 };
-// 8-bit operands: the instruction's lane holds channels 16 h .. and 32 + 16 h ..
-// of the step (its scale is still that of block h).
+// 8-bit operands: the instruction's lane holds channels 16 g .. and 64 + 16 g ..
+// (its scale is still that of block g); decoded, 32 g .. as with 4 bits.
 template <bool DEC> struct Frag<POLESTAR_MXFP8, DEC> {
     uint4 c[2];
-    __device__ __forceinline__ void load(const uint8_t* row, int step, int h) {
-        const uint8_t* p = row + 64 * step;
-        c[0] = ld16(p + (DEC ? 32 * h : 16 * h));
-        c[1] = ld16(p + (DEC ? 32 * h + 16 : 32 + 16 * h));
+    __device__ __forceinline__ void load(const char* tile, int r, int g) {
+        c[0] = ld16(tile + r * 128 + LdsRow<POLESTAR_MXFP8>::chunk(r, DEC ? 2 * g : g));
+        c[1] = ld16(tile + r * 128 + LdsRow<POLESTAR_MXFP8>::chunk(r, DEC ? 2 * g + 1 : 4 + g));
     }
     __device__ __forceinline__ intx8 codes() const {
         return intx8{static_cast<int>(c[0].x), static_cast<int>(c[0].y), static_cast<int>(c[0].z), static_cast<int>(c[0].w),
@@ -58,71 +80,396 @@ template <bool DEC> struct Frag<POLESTAR_MXFP8, DEC> {
     }
 };
 
-// A wave per 32 x 32 outputs, operands straight from memory.  grid (rows / 64, n_out / 64)
-template <int FMT, bool BF16>
-__global__ __launch_bounds__(256) void mx_gemm_kernel(MxGemmArgs g) {
+constexpr int kMxTileThreads = 512;                      // eight waves, two per SIMD
+constexpr int kMxBand = 4;                               // row tiles per band of the launch order
+constexpr int kMxCus = 256;
+
+// Transfers into LDS, 16 or 12 bytes per lane, from a buffer of `bytes` bytes at
+// base: a lane's offset is one register, the K tile's a scalar; the lanes land one
+// after another from lds on.  Written out, because the compiler waits for every
+// transfer that it knows of before it reads LDS; the waits are the kernel's own
+// (mx_wait_vm before the barrier that hands a slot over).
+typedef uint32_t MxBuffer __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ MxBuffer mx_buffer(const void* base, uint32_t bytes) {
+    const uint64_t p = reinterpret_cast<uint64_t>(base);
+    return MxBuffer{uniform(static_cast<uint32_t>(p)), uniform(static_cast<uint32_t>(p >> 32)), uniform(bytes), 0x00027000u};
+}
+__device__ __forceinline__ uint32_t lds_offset(const char* p) {
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
+}
+#define PS_MX_DMA(OP)                                                                      \
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" OP " %1, %2, %3 offen lds"             \
+                 :: "s"(uniform(lds_offset(lds))), "v"(lane_off), "s"(b), "s"(uniform(off)) : "memory")
+__device__ __forceinline__ void mx_dma16(MxBuffer b, uint32_t lane_off, uint32_t off, const char* lds) {
+    PS_MX_DMA("buffer_load_dwordx4");
+}
+__device__ __forceinline__ void mx_dma12(MxBuffer b, uint32_t lane_off, uint32_t off, const char* lds) {
+    PS_MX_DMA("buffer_load_dwordx3");
+}
+#undef PS_MX_DMA
+// s_waitcnt immediates: at most n vector-memory operations outstanding / LDS reads done
+constexpr int mx_wait_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+constexpr int kMxWaitLgkm0 = 15 | (3 << 14) | (7 << 4);
+
+// LDS: slots of a K tile's codes, as many as fit, three or four, beside two
+// buffers of the scales of as many K tiles.
+constexpr int mx_slot_bytes(int fmt, int mi, int nj) { return 32 * mi * (fmt == POLESTAR_MXFP8 ? 128 : 64) + 64 * nj * 64; }
+constexpr int mx_slots(int fmt, int mi, int nj) {
+    return 4 * (mx_slot_bytes(fmt, mi, nj) + 8 * (32 * mi + 64 * nj)) <= 160 * 1024 ? 4 : 3;
+}
+
+// Workgroup blk -> (split, row tile, column tile): consecutive workgroups go to
+// different XCDs, so the ids are first regrouped per XCD, and each XCD walks
+// bands of row tiles column by column, which keeps the rows and weights that its
+// compute units share in its own L2.
+__device__ __forceinline__ void mx_tile_coords(const MxGemmArgs& g, int blk, int& split, int& rt, int& ct) {
+    const int ntiles = g.row_tiles * g.col_tiles, nb = ntiles * g.ksplit;
+    const int xcd = blk & 7;
+    const int bid = xcd * (nb >> 3) + min(xcd, nb & 7) + (blk >> 3);
+    split = bid / ntiles;
+    const int tl = bid - split * ntiles;
+    const int band = tl / (kMxBand * g.col_tiles);
+    const int rows_here = min(kMxBand, g.row_tiles - band * kMxBand);
+    const int in = tl - band * kMxBand * g.col_tiles;
+    ct = in / rows_here;
+    rt = band * kMxBand + (in - ct * rows_here);
+}
+
+// 32 MI rows x 64 NJ outputs per workgroup: eight waves in a 2 x 4 grid of MI x NJ
+// tiles of the 16x16x128 scaled instruction (DEC: four 16x16x32 bf16 ones), K in
+// tiles of 128 channels, codes and scales by DMA into NS LDS slots, one barrier
+// per K tile.
+template <int FMT, bool BF16, int MI, int NJ>
+__global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     constexpr bool DEC = FMT == POLESTAR_MXFP8 && !BF16;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int i = lane & 31, h = lane >> 5;
-    const long m = static_cast<long>(blockIdx.x) * 64 + 32 * (w & 1) + i;
-    const int n0 = blockIdx.y * 64 + 32 * (w >> 1);
-    const long mr = min(m, g.rows - 1);                  // rows and columns past the end: the last one, not stored
-    const int nr = min(n0 + i, g.n_out - 1);
-    const uint8_t* xr = g.x + static_cast<size_t>(mr) * (g.n_in / 8) * Mx<FMT>::kBits;
-    const uint8_t* xsr = g.xs + static_cast<size_t>(mr) * (g.n_in / 32);
-    const uint8_t* wr = g.w + static_cast<size_t>(nr) * (g.n_in / 2);
-    const uint8_t* wsr = g.ws + static_cast<size_t>(nr) * (g.n_in / 32);
-    floatx16 acc;
+    constexpr int BM = 32 * MI, BN = 64 * NJ;
+    constexpr int XB = LdsRow<FMT>::kBytes, WB = LdsRow<POLESTAR_MXFP4>::kBytes;
+    constexpr int XG = BM * XB / 1024, WG = BN * WB / 1024, SG = (BM + BN) / 64;   // DMA groups of a K tile
+    constexpr int XI = (XG + 7) / 8, WI = (WG + 7) / 8;  // instructions per wave
+    constexpr int ND = XI + WI;
+    constexpr int NS = mx_slots(FMT, MI, NJ);
+    static_assert(SG <= 8, "a wave per group of scales");
+    constexpr int W0 = BM * XB, SLOT = mx_slot_bytes(FMT, MI, NJ);   // a slot: rows, weights
+    constexpr int SB = 4 * NS, SBUF = SB * (BM + BN);    // a row's scales of NS K tiles
+    __shared__ __align__(16) char l0[SLOT], l1[SLOT], l2[SLOT], l3[NS > 3 ? SLOT : 1], sc[2 * SBUF];
+
+    int split, rt, ct;
+    mx_tile_coords(g, blockIdx.x, split, rt, ct);
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = w & 1, wn = w >> 1;
+    const int r = lane & 15, grp = lane >> 4;
+    const long m0 = static_cast<long>(rt) * BM;
+    const int n0 = ct * BN;
+    const int kt0 = split * g.steps;
+    const int nkt = min(g.steps, g.n_in / 128 - kt0);
+
+    // DMA sources.  The buffers end with the tile's last row: what lies behind it
+    // (rows and columns past the end, scales behind the last K tile) reads as 0.  A
+    // group past the last (few rows): the last group again, the same bytes.
+    const uint32_t xrow = static_cast<uint32_t>(g.n_in / 8) * Mx<FMT>::kBits, wrow = g.n_in / 2, srow = g.n_in / 32;
+    const uint32_t mrows = static_cast<uint32_t>(min(g.rows - m0, static_cast<long>(BM))), nrows = min(g.n_out - n0, BN);
+    const MxBuffer xbuf = mx_buffer(g.x + static_cast<size_t>(m0) * xrow, mrows * xrow);
+    const MxBuffer wbuf = mx_buffer(g.w + static_cast<size_t>(n0) * wrow, nrows * wrow);
+    constexpr int XR = 1024 / XB, WR = 1024 / WB;        // rows of a group
+    const int xg = min(w, XG - 1), wg = min(w, WG - 1), xr = xg * XR + lane / (XB / 16), wr = wg * WR + lane / (WB / 16);
+    const uint32_t xsrc = xr * xrow + LdsRow<FMT>::chunk(xr, lane % (XB / 16));   // (the swizzle repeats with the groups)
+    const uint32_t wsrc = wr * wrow + LdsRow<POLESTAR_MXFP4>::chunk(wr, lane % (WB / 16));
+    // DMA instructions d0 .. d0 + n - 1 of K tile kt (past the split: its last one again)
+    auto issue = [&](int d0, int n, int kt, const char* slot) {
+        const uint32_t k = kt0 + min(kt, nkt - 1);
 #pragma unroll
-    for (int j = 0; j < 16; ++j) acc[j] = 0.f;
-    for (int s = 0; s < g.n_in / 64; ++s) {
-        Frag<FMT, DEC> fx;
-        Frag<POLESTAR_MXFP4, DEC> fw;
-        fx.load(xr, s, h);
-        fw.load(wr, s, h);
-        const uint32_t sx = xsr[2 * s + h], sw = wsr[2 * s + h];
+        for (int d = d0; d < d0 + n; ++d) {
+            if (d < XI) mx_dma16(xbuf, xsrc, k * XB + 8 * d * XR * xrow, slot + (xg + 8 * d) * 1024);
+            else if (d < ND)
+                mx_dma16(wbuf, wsrc, k * WB + 8 * (d - XI) * WR * wrow, slot + W0 + (wg + 8 * (d - XI)) * 1024);
+        }
+    };
+    // Scales, NS K tiles at a time: 64 rows of x or of w per wave.  (One K tile's
+    // four bytes at a time are a cache line each too, and took a quarter of the time.)
+    const int sg = min(w, SG - 1);
+    const bool of_x = sg < BM / 64;
+    const MxBuffer sbuf = of_x ? mx_buffer(g.xs + static_cast<size_t>(m0) * srow, mrows * srow)
+                               : mx_buffer(g.ws + static_cast<size_t>(n0) * srow, nrows * srow);
+    const uint32_t ssrc = static_cast<uint32_t>(of_x ? 64 * sg + lane : 64 * sg + lane - BM) * srow;
+    auto issue_scales = [&](int kt, int buf) {
+        if constexpr (NS == 4) mx_dma16(sbuf, ssrc, 4 * (kt0 + kt), sc + buf + 64 * SB * sg);
+        else mx_dma12(sbuf, ssrc, 4 * (kt0 + kt), sc + buf + 64 * SB * sg);
+    };
+
+    // Row fragments: of two K tiles, or for the largest tile (kRing: two would not
+    // fit the registers) four, each replaced right after its use by the one four
+    // row tiles on, of this K tile or the next.
+    constexpr bool kRing = MI == 8;
+    constexpr int NB = kRing ? 1 : 2, NX = kRing ? 4 : MI;
+    static_assert(kRing || NS % 2 == 0, "two register sets, in turn");
+    Frag<FMT, DEC> fx[NB][NX];
+    Frag<POLESTAR_MXFP4, DEC> fw[NB][NJ], fwn[NJ];
+    uint32_t sx[NB][NX], sw[NB][NJ], swn[NJ];            // scale bytes
+    const char* const xsc = sc + (16 * MI * wm + r) * SB + grp;
+    const char* const wsc = sc + (BM + 16 * NJ * wn + r) * SB + grp;
+    // fragments and scales (at so in the buffers) of a K tile
+    auto read_x = [&](const char* slot, int so, int set, int j) {
+        fx[set][j % NX].load(slot + 16 * (MI * wm + j) * XB, r, grp);
+        sx[set][j % NX] = *reinterpret_cast<const uint8_t*>(xsc + so + 16 * SB * j);
+    };
+    auto read_w = [&](const char* slot, int so, Frag<POLESTAR_MXFP4, DEC>* f, uint32_t* s) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            f[j].load(slot + W0 + 16 * (NJ * wn + j) * WB, r, grp);
+            s[j] = *reinterpret_cast<const uint8_t*>(wsc + so + 16 * SB * j);
+        }
+    };
+    floatx4 acc[MI][NJ];
+#pragma unroll
+    for (int a = 0; a < MI; ++a)
+#pragma unroll
+        for (int b = 0; b < NJ; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto mma = [&](int set, int a) {
         if constexpr (DEC) {
-            uint4 ax[4], aw[4];
-            fx.decode(ax, mx_scale(sx));
-            fw.decode(aw, mx_scale(sw));
+            uint4 dx[4];
+            fx[set][a % NX].decode(dx, mx_scale(sx[set][a % NX]));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc = Mma32<true>::step(aw[j], ax[j], acc);
+            for (int b = 0; b < NJ; ++b) {
+                uint4 dw[4];
+                fw[set][b].decode(dw, mx_scale(sw[set][b]));
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[a][b] = mfma_bf16(dw[t], dx[t], acc[a][b]);
+            }
         } else {
-            acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fw.codes(), fx.codes(), acc, Mx<POLESTAR_MXFP4>::kMfma,
-                                                                  Mx<FMT>::kMfma, 0, sw, 0, sx);
+#pragma unroll
+            for (int b = 0; b < NJ; ++b)
+                acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                    fw[set][b].codes(), fx[set][a % NX].codes(), acc[a][b], Mx<POLESTAR_MXFP4>::kMfma, Mx<FMT>::kMfma, 0,
+                    sw[set][b], 0, sx[set][a % NX]);
+        }
+    };
+
+    issue_scales(0, 0);
+    issue(0, ND, 0, l0);
+    issue(0, ND, 1, l1);
+    issue(0, ND, 2, l2);
+    if constexpr (NS > 3) issue(0, ND, 3, l3);
+    __builtin_amdgcn_s_waitcnt(mx_wait_vm((NS - 1) * ND));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_w(l0, 0, fw[0], sw[0]);
+#pragma unroll
+    for (int a = 0; a < NX; ++a) read_x(l0, 0, 0, a);
+    // K tile T in slot U (its first fragments in registers), T + 1 in X.  The barrier
+    // is for this wave's reads of U and its DMA of T + 1: behind it T + 1 may be read
+    // and U takes T + NS, a few instructions per row tile.
+    constexpr int DPR = kRing ? (ND + MI - 6) / (MI - 5) : (ND + MI - 1) / MI;
+    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+    auto sync = [&] {
+        fence();
+        __builtin_amdgcn_s_waitcnt(mx_wait_vm((NS - 2) * ND) & kMxWaitLgkm0);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        fence();
+    };
+    auto ktile = [&](auto set, int t, const char* u, const char* x, int su, int so) {
+        constexpr int S = kRing ? 0 : decltype(set)::value;
+        if constexpr (kRing) {
+#pragma unroll
+            for (int a = 0; a < MI; ++a) {
+                mma(0, a);
+                if (a == MI - 4) {
+                    sync();
+                    read_w(x, so, fwn, swn);
+                }
+                fence();
+                if (a < MI - 4) read_x(u, su, 0, a + 4);
+                else read_x(x, so, 0, a + 4 - MI);
+                if (a > MI - 4) issue((a - MI + 3) * DPR, DPR, t + NS, u);
+                fence();
+            }
+#pragma unroll
+            for (int b = 0; b < NJ; ++b) {
+                fw[0][b] = fwn[b];
+                sw[0][b] = swn[b];
+            }
+        } else {
+            sync();
+            read_w(x, so, fw[1 - S], sw[1 - S]);
+#pragma unroll
+            for (int a = 0; a < MI; ++a) read_x(x, so, 1 - S, a);
+            fence();
+#pragma unroll
+            for (int a = 0; a < MI; ++a) {
+                mma(S, a);
+                issue(a * DPR, DPR, t + NS, u);
+                fence();
+            }
+        }
+    };
+    using Set0 = std::integral_constant<int, 0>;
+    using Set1 = std::integral_constant<int, 1>;
+    int kt = 0, buf = 0;                                 // buf: the scales of K tiles kt .. kt + NS - 1
+    for (; kt + NS <= nkt; kt += NS, buf ^= SBUF) {
+        ktile(Set0{}, kt, l0, l1, buf, buf + 4);
+        issue_scales(kt + NS, buf ^ SBUF);               // landed by the last sync of this round
+        ktile(Set1{}, kt + 1, l1, l2, buf + 4, buf + 8);
+        if constexpr (NS == 3) {
+            ktile(Set0{}, kt + 2, l2, l0, buf + 8, buf ^ SBUF);
+        } else {
+            ktile(Set0{}, kt + 2, l2, l3, buf + 8, buf + 12);
+            ktile(Set1{}, kt + 3, l3, l0, buf + 12, buf ^ SBUF);
         }
     }
-    if (m >= g.rows) return;
+    if (kt < nkt) ktile(Set0{}, kt, l0, l1, buf, buf + 4);
+    if (kt + 1 < nkt) ktile(Set1{}, kt + 1, l1, l2, buf + 4, buf + 8);
+    if constexpr (NS == 4)
+        if (kt + 2 < nkt) ktile(Set0{}, kt + 2, l2, l3, buf + 8, buf + 12);
+    __builtin_amdgcn_s_waitcnt(0);                       // every DMA (the re-read tail too) has landed
+    __syncthreads();                                     // and every wave is done with the slots
+
+    // lane: row r of its tile, outputs 4 grp .. + 3
+    const int nw = n0 + 16 * NJ * wn;
+    if (g.ksplit > 1) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = n0 + 8 * j + 4 * h;
-        if (n >= g.n_out) break;
-        const size_t at = static_cast<size_t>(m) * g.n_out + n;
-        if constexpr (BF16)
-            *reinterpret_cast<uint2*>(g.y + 2 * at) =
-                make_uint2(pack_bf16x2(acc[4 * j], acc[4 * j + 1]), pack_bf16x2(acc[4 * j + 2], acc[4 * j + 3]));
-        else
-            *reinterpret_cast<float4*>(g.y + 4 * at) = make_float4(acc[4 * j], acc[4 * j + 1], acc[4 * j + 2], acc[4 * j + 3]);
+        for (int a = 0; a < MI; ++a) {
+            const long m = m0 + 16 * (MI * wm + a) + r;
+            if (m >= g.rows) continue;
+            float* p = g.part + (static_cast<size_t>(split) * g.rows + m) * g.n_out;
+#pragma unroll
+            for (int b = 0; b < NJ; ++b) {
+                const int n = nw + 16 * b + 4 * grp;
+                if (n < g.n_out) *reinterpret_cast<floatx4*>(p + n) = acc[a][b];
+            }
+        }
+        return;
+    }
+    // through LDS, 16 rows of the wave at a time in a region of its own, then 16
+    // bytes of a row per lane
+    constexpr int ES = BF16 ? 2 : 4;
+    constexpr int EP = 16 * NJ * ES + 16;                // bytes of a staged row
+    constexpr int CPR = NJ * ES;                         // 16-byte chunks of a row
+    static_assert(3 * 16 * EP <= SLOT, "three waves' rows fit a slot");
+    char* ep = (w % 3 == 0 ? l0 : w % 3 == 1 ? l1 : l2) + (w / 3) * 16 * EP;
+#pragma unroll
+    for (int a = 0; a < MI; ++a) {
+#pragma unroll
+        for (int b = 0; b < NJ; ++b) {
+            char* d = ep + r * EP + (16 * b + 4 * grp) * ES;
+            const floatx4& v = acc[a][b];
+            if constexpr (BF16)
+                *reinterpret_cast<uint2*>(d) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
+            else
+                *reinterpret_cast<floatx4*>(d) = v;
+        }
+        __builtin_amdgcn_s_waitcnt(kMxWaitLgkm0);
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < (16 * CPR + 63) / 64; ++q) {
+            const int at = 64 * q + lane, c = at % CPR;
+            const long m = m0 + 16 * (MI * wm + a) + at / CPR;
+            const int n = nw + c * (16 / ES);
+            if (at < 16 * CPR && m < g.rows && n < g.n_out)
+                st16(g.y + (static_cast<size_t>(m) * g.n_out + n) * ES, ld16(ep + at / CPR * EP + 16 * c));
+        }
+        __builtin_amdgcn_s_waitcnt(kMxWaitLgkm0);
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// The splits' partials, added in order; four outputs per thread.
+template <bool BF16>
+__global__ __launch_bounds__(256) void mx_reduce_kernel(const float* __restrict__ part, int ksplit, long n4,
+                                                        char* __restrict__ y) {
+    const long i = static_cast<long>(blockIdx.x) * 256 + threadIdx.x;
+    if (i >= n4) return;
+    const float4* p = reinterpret_cast<const float4*>(part) + i;
+    float4 v = p[0];
+    for (int s = 1; s < ksplit; ++s) {
+        const float4 e = p[s * n4];
+        v = make_float4(v.x + e.x, v.y + e.y, v.z + e.z, v.w + e.w);
+    }
+    if constexpr (BF16) reinterpret_cast<uint2*>(y)[i] = make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w));
+    else reinterpret_cast<float4*>(y)[i] = v;
+}
+
+// The tile shapes (MI, NJ); the decoding form has no registers for the two largest.
+constexpr bool mx_has_tile(int fmt, bool bf16, int mi, int nj) { return mi * nj <= 8 || fmt == POLESTAR_MXFP4 || bf16; }
+#define PS_MX_SHAPES(X) X(8, 4) X(4, 4) X(4, 2) X(2, 4) X(2, 2)
+
+struct MxPlan {
+    int mi, nj, ksplit, steps;
+    size_t ws_bytes;
+};
+
+// Tile shape and K split with the least estimated time: rounds of one workgroup
+// per CU, each its K tiles and a fixed cost, and for a split the partials'
+// way through memory.
+MxPlan mx_plan(int x_fmt, bool bf16, long rows, int n_out, int n_in) {
+    static constexpr struct { int mi, nj; double kt; } shapes[] = {{8, 4, 1.5}, {4, 4, 0.9}, {4, 2, 0.55}, {2, 4, 0.6}, {2, 2, 0.36}};
+    const int nkt = n_in / 128;
+    MxPlan p{};
+    double best = 1e30;
+    for (const auto& s : shapes) {
+        if (!mx_has_tile(x_fmt, bf16, s.mi, s.nj)) continue;
+        const long tiles = ((rows + 32 * s.mi - 1) / (32 * s.mi)) * ceil_div(n_out, 64 * s.nj);
+        for (int ks = 1; ks <= 16 && ks <= nkt; ++ks) {
+            const int steps = ceil_div(nkt, ks);
+            if (ceil_div(nkt, steps) != ks) continue;
+            if (ks > 1 && (tiles * (ks - 1) >= kMxCus || steps < 4)) break;
+            const double rounds = static_cast<double>((tiles * ks + kMxCus - 1) / kMxCus);
+            const double cost = rounds * (steps * s.kt + 4.0) + (ks > 1 ? 4.0 + 4.0 * ks * rows * n_out * 0.4e-6 : 0.0);
+            if (cost < best) {
+                best = cost;
+                p = MxPlan{s.mi, s.nj, ks, steps, ks > 1 ? 4 * static_cast<size_t>(ks) * rows * n_out : 0};
+            }
+        }
+    }
+    return p;
+}
+
+template <int FMT, bool BF16>
+void mx_launch(const MxPlan& p, const MxGemmArgs& g, hipStream_t stream) {
+    const dim3 grid(g.row_tiles * g.col_tiles * g.ksplit), block(kMxTileThreads);
+    switch (10 * p.mi + p.nj) {
+#define PS_CASE(MI, NJ) \
+        case 10 * MI + NJ:                                                                                   \
+            if constexpr (mx_has_tile(FMT, BF16, MI, NJ))                                                    \
+                hipLaunchKernelGGL((mx_tile_kernel<FMT, BF16, MI, NJ>), grid, block, 0, stream, g);          \
+            break;
+        PS_MX_SHAPES(PS_CASE)
+#undef PS_CASE
+    }
+    if (g.ksplit > 1) {
+        const long n4 = g.rows * (g.n_out / 4);
+        hipLaunchKernelGGL((mx_reduce_kernel<BF16>), dim3(ceil_div(n4, 256)), dim3(256), 0, stream, g.part, g.ksplit, n4, g.y);
     }
 }
 
 bool mx_fmt_ok(int fmt) { return fmt == POLESTAR_MXFP4 || fmt == POLESTAR_MXFP8; }
 
-size_t mx_linear_ws(int x_fmt, polestar_dtype dtype, long rows, int n_out, int n_in) { return 0; }
+size_t mx_linear_ws(int x_fmt, polestar_dtype dtype, long rows, int n_out, int n_in) {
+    return mx_plan(x_fmt, dtype == POLESTAR_BF16, rows, n_out, n_in).ws_bytes;
+}
 
-polestar_status mx_gemm_run(int x_fmt, polestar_dtype dtype, const MxGemmArgs& g, hipStream_t stream) {
-    const dim3 grid(static_cast<unsigned>((g.rows + 63) / 64), ceil_div(g.n_out, 64));
+polestar_status mx_gemm_run(int x_fmt, polestar_dtype dtype, MxGemmArgs g, void* workspace, hipStream_t stream) {
     const bool bf16 = dtype == POLESTAR_BF16;
-#define PS_GEMM(F, BF) hipLaunchKernelGGL((mx_gemm_kernel<F, BF>), grid, dim3(256), 0, stream, g)
-    if (x_fmt == POLESTAR_MXFP4) { if (bf16) PS_GEMM(POLESTAR_MXFP4, true); else PS_GEMM(POLESTAR_MXFP4, false); }
-    else { if (bf16) PS_GEMM(POLESTAR_MXFP8, true); else PS_GEMM(POLESTAR_MXFP8, false); }
-#undef PS_GEMM
+    const MxPlan p = mx_plan(x_fmt, bf16, g.rows, g.n_out, g.n_in);
+    g.part = static_cast<float*>(workspace);
+    g.ksplit = p.ksplit;
+    g.steps = p.steps;
+    g.row_tiles = ceil_div(g.rows, 32 * p.mi);
+    g.col_tiles = ceil_div(g.n_out, 64 * p.nj);
+    if (x_fmt == POLESTAR_MXFP4) {
+        if (bf16) mx_launch<POLESTAR_MXFP4, true>(p, g, stream);
+        else mx_launch<POLESTAR_MXFP4, false>(p, g, stream);
+    } else {
+        if (bf16) mx_launch<POLESTAR_MXFP8, true>(p, g, stream);
+        else mx_launch<POLESTAR_MXFP8, false>(p, g, stream);
+    }
     return launch_status();
 }
 
 // Rows and outputs that the kernels' indices hold.
 bool mx_shape_ok(long rows, int n_out, int n_in) {
-    return n_in % 128 == 0 && n_out % 16 == 0 && rows <= (1L << 24) && n_out <= (1 << 22);
+    return n_in % 128 == 0 && n_out % 16 == 0 && rows <= (1L << 24) && n_out <= (1 << 22) && n_in <= (1 << 22);
 }
 
 // Workspace of the quantized rows: codes, then scales.
@@ -155,8 +502,16 @@ extern "C" polestar_status polestar_mx_linear(int x_fmt, polestar_dtype dtype, l
     if (rows == 0) return POLESTAR_OK;
     const size_t need = mx_linear_ws(x_fmt, dtype, rows, n_out, n_in);
     if (workspace_bytes < need || (need > 0 && !workspace)) return POLESTAR_ERR_WORKSPACE;
-    const MxGemmArgs g{x_codes, x_scales, w_codes, w_scales, static_cast<char*>(y), rows, n_out, n_in};
-    return mx_gemm_run(x_fmt, dtype, g, stream);
+    MxGemmArgs g{};
+    g.x = x_codes;
+    g.xs = x_scales;
+    g.w = w_codes;
+    g.ws = w_scales;
+    g.y = static_cast<char*>(y);
+    g.rows = rows;
+    g.n_out = n_out;
+    g.n_in = n_in;
+    return mx_gemm_run(x_fmt, dtype, g, workspace, stream);
 }
 
 extern "C" size_t polestar_mx_quantize_linear_workspace_size(int x_fmt, polestar_dtype dtype, int batch, int n_rows,
