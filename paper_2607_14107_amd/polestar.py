@@ -24,6 +24,7 @@ LIB_PATH = os.environ.get("POLESTAR_LIB") or os.path.join(PKG, "libpolestar.so")
 
 OK = 0
 STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported", 3: "launch failed", 4: "workspace too small"}
+STATUS_WORKSPACE = 4
 FP32, BF16 = 0, 1
 MXFP4, MXFP8 = 0, 1
 CODECS = {"mxfp4": MXFP4, "mxfp8": MXFP8}
@@ -599,35 +600,55 @@ def codec_gather(fmt: int, codes: torch.Tensor, scales: torch.Tensor, idx: torch
 # a layer's forward in the microscaling formats (include/polestar_mx.h)
 # ---------------------------------------------------------------------------
 
-def _mx_device(*tensors) -> torch.device:
-    """The one device of the given tensors, which has to be the current one."""
-    dev = None
+def _mx_device(*tensors) -> int:
+    """The index of the one device of the given tensors, which has to be the current one."""
+    dev = tensors[0].get_device()
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("tensor must be on the GPU")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
+        if t is not None and t.get_device() != dev:
             raise ValueError("tensors are on different devices")
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+    if dev < 0:
+        raise ValueError("tensor must be on the GPU")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"tensors are on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
     return dev
 
 
-def _mx_empty(shape, dtype, device, stream) -> torch.Tensor:
+def _mx_ptr(t: torch.Tensor | None, dtype: torch.dtype) -> int | None:
+    """_ptr for a tensor whose device is known."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return t.data_ptr()
+
+
+def _mx_stream(dev: int, stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _mx_empty(shape, dtype, dev: int, stream) -> torch.Tensor:
     """A new tensor for work on `stream`: kept from reuse until that is done where it is not the current stream."""
-    t = torch.empty(shape, dtype=dtype, device=device)
+    t = torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
     if stream is not None and stream != torch.cuda.current_stream():
         t.record_stream(stream)
     return t
 
 
-def _mx_workspace(nbytes: int, device, ws: torch.Tensor | None, stream):
-    if nbytes == 0 or (ws is not None and ws.numel() * ws.element_size() >= nbytes):
-        return ws
-    return _mx_empty(nbytes, torch.uint8, device, stream)
+def _mx_call(name: str, args: tuple, size, ws: torch.Tensor | None, dev: int, stream) -> None:
+    """The call `name` with args, a workspace and the stream; the workspace is made where none is given or the
+    given one is too small (size(): what the call needs)."""
+    f = getattr(lib(), name)
+    st = _mx_stream(dev, stream)
+    status = STATUS_WORKSPACE
+    if ws is not None:
+        status = f(*args, _mx_ptr(ws, ws.dtype), ws.numel() * ws.element_size(), st)
+    if status == STATUS_WORKSPACE:
+        nbytes = size()
+        ws = _mx_empty(nbytes, torch.uint8, dev, stream) if nbytes else None
+        status = f(*args, None if ws is None else ws.data_ptr(), nbytes, st)
+    _check(name, status)
 
 
 def _mx_codes(fmt: int, codes: torch.Tensor, scales: torch.Tensor, what: str) -> int:
@@ -672,20 +693,20 @@ def mx_quantize(fmt: int, x: torch.Tensor, row_start: int = 0, n_rows: int | Non
     if _mx_codes(fmt, codes, scales, "mx_quantize") != n or scales.numel() * 32 != b * n_rows * n:
         raise ValueError("mx_quantize: shapes do not match")
     _check("polestar_mx_quantize", lib().polestar_mx_quantize(
-        fmt, _dtype_code(x), b, seq, n, row_start, n_rows, _ptr(x), _ptr(codes, torch.uint8),
-        _ptr(scales, torch.uint8), _stream(stream)))
+        fmt, _dtype_code(x), b, seq, n, row_start, n_rows, _mx_ptr(x, x.dtype), _mx_ptr(codes, torch.uint8),
+        _mx_ptr(scales, torch.uint8), _mx_stream(dev, stream)))
     return codes, scales
 
 
 def mx_dequantize(fmt: int, codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None) -> torch.Tensor:
     """The values of codes [..., row bytes] and scales [..., n / 32] into out [..., n] (float32 or bfloat16)."""
     n = _mx_codes(fmt, codes, scales, "mx_dequantize")
-    if tuple(out.shape) != (*codes.shape[:-1], n):
+    if out.shape[-1] != n or out.shape[:-1] != codes.shape[:-1]:
         raise ValueError("mx_dequantize: shapes do not match")
-    _mx_device(codes, scales, out)
+    dev = _mx_device(codes, scales, out)
     _check("polestar_mx_dequantize", lib().polestar_mx_dequantize(
-        fmt, _dtype_code(out), out.numel() // n if n else 0, n, _ptr(codes, torch.uint8), _ptr(scales, torch.uint8),
-        _ptr(out), _stream(stream)))
+        fmt, _dtype_code(out), out.numel() // n if n else 0, n, _mx_ptr(codes, torch.uint8),
+        _mx_ptr(scales, torch.uint8), _mx_ptr(out, out.dtype), _mx_stream(dev, stream)))
     return out
 
 
@@ -700,15 +721,14 @@ def mx_linear(x_fmt: int, x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes
     n_in = _mx_codes(x_fmt, x_codes, x_scales, "mx_linear")
     n_out = w_codes.shape[0]
     if (_mx_codes(MXFP4, w_codes, w_scales, "mx_linear") != n_in or w_codes.dim() != 2
-            or tuple(y.shape) != (*x_codes.shape[:-1], n_out)):
+            or y.shape[-1] != n_out or y.shape[:-1] != x_codes.shape[:-1]):
         raise ValueError("mx_linear: shapes do not match")
     dev = _mx_device(x_codes, x_scales, w_codes, w_scales, y, workspace)
     rows, dt = y.numel() // n_out, _dtype_code(y)
-    ws = _mx_workspace(mx_linear_workspace_size(x_fmt, dt, rows, n_out, n_in), dev, workspace, stream)
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check("polestar_mx_linear", lib().polestar_mx_linear(
-        x_fmt, dt, rows, n_in, n_out, _ptr(x_codes, torch.uint8), _ptr(x_scales, torch.uint8),
-        _ptr(w_codes, torch.uint8), _ptr(w_scales, torch.uint8), _ptr(y), _ptr(ws), nbytes, _stream(stream)))
+    _mx_call("polestar_mx_linear", (
+        x_fmt, dt, rows, n_in, n_out, _mx_ptr(x_codes, torch.uint8), _mx_ptr(x_scales, torch.uint8),
+        _mx_ptr(w_codes, torch.uint8), _mx_ptr(w_scales, torch.uint8), _mx_ptr(y, y.dtype)),
+        lambda: mx_linear_workspace_size(x_fmt, dt, rows, n_out, n_in), workspace, dev, stream)
     return y
 
 
@@ -724,15 +744,14 @@ def mx_quantize_linear(x_fmt: int, x: torch.Tensor, row_start: int, n_rows: int,
     b, seq, n_in = x.shape
     n_out = w_codes.shape[0]
     if (_mx_codes(MXFP4, w_codes, w_scales, "mx_quantize_linear") != n_in or w_codes.dim() != 2
-            or tuple(y.shape) != (b, n_rows, n_out)):
+            or y.shape != (b, n_rows, n_out)):
         raise ValueError("mx_quantize_linear: shapes do not match")
     dev = _mx_device(x, w_codes, w_scales, y, workspace)
     dt = _dtype_code(x)
-    ws = _mx_workspace(mx_quantize_linear_workspace_size(x_fmt, dt, b, n_rows, n_out, n_in), dev, workspace, stream)
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check("polestar_mx_quantize_linear", lib().polestar_mx_quantize_linear(
-        x_fmt, dt, b, seq, n_in, n_out, row_start, n_rows, _ptr(x), _ptr(w_codes, torch.uint8),
-        _ptr(w_scales, torch.uint8), _ptr(y, x.dtype), _ptr(ws), nbytes, _stream(stream)))
+    _mx_call("polestar_mx_quantize_linear", (
+        x_fmt, dt, b, seq, n_in, n_out, row_start, n_rows, _mx_ptr(x, x.dtype), _mx_ptr(w_codes, torch.uint8),
+        _mx_ptr(w_scales, torch.uint8), _mx_ptr(y, x.dtype)),
+        lambda: mx_quantize_linear_workspace_size(x_fmt, dt, b, n_rows, n_out, n_in), workspace, dev, stream)
     return y
 
 
@@ -744,13 +763,14 @@ def residual_rmsnorm_mx(fmt: int, x: torch.Tensor, y: torch.Tensor | None, x_out
     d = x.shape[-1]
     if (_mx_codes(fmt, codes, scales, "residual_rmsnorm_mx") != d or codes.shape[:-1] != x.shape[:-1]
             or (y is not None and (y.shape != x.shape or x_out is None))
-            or (x_out is not None and x_out.shape != x.shape) or (gain is not None and tuple(gain.shape) != (d,))):
+            or (x_out is not None and x_out.shape != x.shape) or (gain is not None and gain.shape != (d,))):
         raise ValueError("residual_rmsnorm_mx: shapes do not match")
-    _mx_device(x, y, x_out, codes, scales, gain)
+    dev = _mx_device(x, y, x_out, codes, scales, gain)
     _check("polestar_residual_rmsnorm_mx", lib().polestar_residual_rmsnorm_mx(
-        fmt, BF16 if y is None else _dtype_code(y), x.numel() // d, d, _ptr(x, torch.float32), _ptr(y),
-        _ptr(gain, torch.float32), float(eps), _ptr(x_out, torch.float32), _ptr(codes, torch.uint8),
-        _ptr(scales, torch.uint8), _stream(stream)))
+        fmt, BF16 if y is None else _dtype_code(y), x.numel() // d, d, _mx_ptr(x, torch.float32),
+        None if y is None else _mx_ptr(y, y.dtype), _mx_ptr(gain, torch.float32), float(eps),
+        _mx_ptr(x_out, torch.float32), _mx_ptr(codes, torch.uint8), _mx_ptr(scales, torch.uint8),
+        _mx_stream(dev, stream)))
 
 
 def _mx_caches(k_codes, k_scales, v_codes, v_scales, what: str):
@@ -769,18 +789,18 @@ def mx_store_kv(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_scale
     product) into caches [batch][n_kv_heads][seq][...], at the positions idx[b][0 .. count[b]) or from row_start on."""
     b, kvh, seq, hd = _mx_caches(k_codes, k_scales, v_codes, v_scales, "mx_store_kv")
     n = k.shape[1]
-    if tuple(k.shape) != (b, n, kvh, hd) or v.shape != k.shape or v.dtype != k.dtype:
+    if k.shape != (b, n, kvh, hd) or v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("mx_store_kv: shapes or dtypes do not match")
-    if (idx is not None and tuple(idx.shape) != (b, n)) or (count is not None and (idx is None or tuple(count.shape) != (b,))):
+    if (idx is not None and idx.shape != (b, n)) or (count is not None and (idx is None or count.shape != (b,))):
         raise ValueError("mx_store_kv: idx must be [batch][n_rows], count [batch] and given with idx")
     rs = _mx_row_stride(k, "mx_store_kv")
-    if n > 0 and _mx_row_stride(v, "mx_store_kv") != rs and n * b > 1:
+    if n * b > 1 and _mx_row_stride(v, "mx_store_kv") != rs:
         raise ValueError("mx_store_kv: k and v differ in row stride")
-    _mx_device(k, v, k_codes, k_scales, v_codes, v_scales, idx, count)
+    dev = _mx_device(k, v, k_codes, k_scales, v_codes, v_scales, idx, count)
     _check("polestar_mx_store_kv", lib().polestar_mx_store_kv(
-        _dtype_code(k), b, seq, kvh, hd, n, k.data_ptr(), v.data_ptr(), rs, _ptr(idx, torch.int32),
-        _ptr(count, torch.int32), row_start, _ptr(k_codes, torch.uint8), _ptr(k_scales, torch.uint8),
-        _ptr(v_codes, torch.uint8), _ptr(v_scales, torch.uint8), _stream(stream)))
+        _dtype_code(k), b, seq, kvh, hd, n, k.data_ptr(), v.data_ptr(), rs, _mx_ptr(idx, torch.int32),
+        _mx_ptr(count, torch.int32), row_start, _mx_ptr(k_codes, torch.uint8), _mx_ptr(k_scales, torch.uint8),
+        _mx_ptr(v_codes, torch.uint8), _mx_ptr(v_scales, torch.uint8), _mx_stream(dev, stream)))
 
 
 def mx_attend_workspace_size(dtype: int, batch: int, seq: int, n_heads: int, n_kv_heads: int, head_dim: int,
@@ -796,20 +816,19 @@ def mx_attend(q: torch.Tensor, k_codes: torch.Tensor, k_scales: torch.Tensor, v_
     (all without kv_len) of K/V caches in MXFP4 [batch][n_kv_heads][seq][...] -> out, q's shape."""
     b, kvh, seq, hd = _mx_caches(k_codes, k_scales, v_codes, v_scales, "mx_attend")
     n, heads = q.shape[1], q.shape[2]
-    if (tuple(q.shape) != (b, n, heads, hd) or (kv_len is not None and tuple(kv_len.shape) != (b,))
-            or (out is not None and out.shape != q.shape) or (lse is not None and tuple(lse.shape) != (b, heads, n))):
+    if (q.shape != (b, n, heads, hd) or (kv_len is not None and kv_len.shape != (b,))
+            or (out is not None and out.shape != q.shape) or (lse is not None and lse.shape != (b, heads, n))):
         raise ValueError("mx_attend: shapes do not match")
+    rs = _mx_row_stride(q, "mx_attend")
     dev = _mx_device(q, k_codes, k_scales, v_codes, v_scales, kv_len, out, lse, workspace)
     dt = _dtype_code(q)
     if out is None:
         out = _mx_empty(q.shape, q.dtype, dev, stream)
-    ws = _mx_workspace(mx_attend_workspace_size(dt, b, seq, heads, kvh, hd, n), dev, workspace, stream)
-    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check("polestar_mx_attend", lib().polestar_mx_attend(
-        dt, b, seq, heads, kvh, hd, n, q.data_ptr(), _mx_row_stride(q, "mx_attend"), _ptr(k_codes, torch.uint8),
-        _ptr(k_scales, torch.uint8), _ptr(v_codes, torch.uint8), _ptr(v_scales, torch.uint8),
-        _ptr(kv_len, torch.int32), float(scale), _ptr(out, q.dtype), _ptr(lse, torch.float32), _ptr(ws), nbytes,
-        _stream(stream)))
+    _mx_call("polestar_mx_attend", (
+        dt, b, seq, heads, kvh, hd, n, q.data_ptr(), rs, _mx_ptr(k_codes, torch.uint8),
+        _mx_ptr(k_scales, torch.uint8), _mx_ptr(v_codes, torch.uint8), _mx_ptr(v_scales, torch.uint8),
+        _mx_ptr(kv_len, torch.int32), float(scale), _mx_ptr(out, q.dtype), _mx_ptr(lse, torch.float32)),
+        lambda: mx_attend_workspace_size(dt, b, seq, heads, kvh, hd, n), workspace, dev, stream)
     return out
 
 
