@@ -6,7 +6,12 @@
 // power of two), an online softmax in base 2 per query (a lane pair), and O^T +=
 // V^T P^T, where S^T's result registers are P^T's operand registers.  V's codes
 // are decoded on their way into LDS and read back transposed
-// (ds_read_b64_tr_b16: four keys of one channel per lane).
+// (ds_read_b64_tr_b16: four keys of one channel per lane).  The next step's codes
+// are loaded before this step's work.
+//
+// The waves of a workgroup take the steps in turn, and where the workgroups do not
+// fill the GPU the keys are split over several; each part's (reference, sum, O) are
+// joined at the end, in LDS and by a second kernel.
 //
 // fp32 queries: q and p are taken as three bf16 terms each, so that the products
 // with the exact keys and values keep 24 bits.
@@ -16,10 +21,10 @@
 namespace ps {
 namespace {
 
-constexpr int kMxAttWaves = 4;
-constexpr int kMxAttThreads = kMxAttWaves * kWave;
 constexpr int kMxKeys = 32;                              // keys of a wave's step
 constexpr int kMxQ = 32;                                 // query vectors of a workgroup
+constexpr int kMxMaxSplits = 64;                         // a lane each in the merge
+constexpr float kMxSlack = 8.f;                          // see the softmax
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
@@ -32,6 +37,9 @@ struct MxAttArgs {
     float* lse;
     float scale2;                                        // scale * log2(e)
     int seq, n_rows, heads, kv_heads, tiles;             // tiles: query tiles of a KV head
+    int splits;
+    float* part;                                         // [batch][kv head][split][query][HD] O, then
+    float2* ml;                                          // [batch][kv head][split][query] (reference, sum)
 };
 
 // Four keys of one channel: lane i of 16 gives the address of four channels of
@@ -60,27 +68,55 @@ __device__ __forceinline__ void split_bf16(const float* v, uint4* o) {
     }
 }
 
-// grid (tiles * kv_heads, batch)
-template <bool BF16, int HD>
-__global__ __launch_bounds__(kMxAttThreads) void mx_attend_kernel(MxAttArgs a) {
+// The codes of a step's 32 keys: lane (key i, half h) holds half of key i's, and of
+// V's rows the chunks that it will decode.
+template <int HD> struct KvStep {
+    static constexpr int NC = HD / 64, VU = HD / 64;
+    uint4 k[NC], v[VU];
+    uint32_t ks, vs[VU];
+    __device__ __forceinline__ void load(const uint8_t* kc, const uint8_t* kss, const uint8_t* vc, const uint8_t* vss,
+                                         int k0, int len, int lane) {
+        constexpr int CT = HD / 32;
+        const size_t kr = min(k0 + (lane & 31), len - 1);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) k[c] = ld16(kc + kr * (HD / 2) + 16 * (2 * c + (lane >> 5)));
+        if constexpr (HD == 128) ks = reinterpret_cast<const uint32_t*>(kss)[kr];
+        else ks = reinterpret_cast<const uint16_t*>(kss)[kr];
+#pragma unroll
+        for (int u = 0; u < VU; ++u) {
+            const int at = u * kWave + lane;
+            const size_t vr = min(k0 + at / CT, len - 1);
+            v[u] = ld16(vc + vr * (HD / 2) + 16 * (at % CT));
+            vs[u] = vss[vr * CT + at % CT];
+        }
+    }
+};
+
+// grid (tiles * kv_heads, splits, batch), NW waves
+template <bool BF16, int HD, int NW>
+__global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
     constexpr int NT = BF16 ? 1 : 3;
     constexpr int ES = Elem<BF16>::kBytes;
     constexpr int NC = HD / 64;                          // 16-byte chunks of a key per lane
     constexpr int CT = HD / 32;                          // channel tiles
     constexpr int kPitch = 2 * HD + 64;                  // bytes of a key's row in LDS
-    __shared__ __align__(16) char vbuf[kMxAttWaves][kMxKeys * kPitch];
-    __shared__ float sm[kMxAttWaves][kMxQ], sl[kMxAttWaves][kMxQ];
-    __shared__ __align__(16) float so[kMxQ][HD + 4];
+    constexpr int kOPitch = 4 * HD + 16;                 // of a query's O
+    constexpr int kV = kMxKeys * kPitch, kO = kMxQ * kOPitch;
+    __shared__ __align__(16) char lds[NW * kV > NW / 2 * kO ? NW * kV : NW / 2 * kO];
+    __shared__ float sm[NW][kMxQ], sl[NW][kMxQ];
 
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int i = lane & 31, h = lane >> 5;
-    const int b = blockIdx.y, g = blockIdx.x / a.tiles, qt = blockIdx.x % a.tiles;
+    const int b = blockIdx.z, g = blockIdx.x / a.tiles, qt = blockIdx.x % a.tiles, split = blockIdx.y;
     const int group = a.heads / a.kv_heads;
     const int len = a.kv_len ? min(max(a.kv_len[b], 0), a.seq) : a.seq;
     const int nq = group * a.n_rows;
     const int qv = qt * kMxQ + i;
     const int qc = min(qv, nq - 1);                      // past the end: the last one, not stored
     const int head = g * group + qc / a.n_rows, row = qc % a.n_rows;
+    // this split's steps, of the sequence's own length
+    const int steps = (len + kMxKeys - 1) / kMxKeys, per = (steps + a.splits - 1) / a.splits;
+    const int s0 = min(split * per, steps), s1 = min(s0 + per, steps);
 
     uint4 q[NC][4][NT];
     {
@@ -101,42 +137,48 @@ __global__ __launch_bounds__(kMxAttThreads) void mx_attend_kernel(MxAttArgs a) {
     }
     const size_t first = (static_cast<size_t>(b) * a.kv_heads + g) * a.seq;   // the head's first key
     const uint8_t* kc = a.kc + first * (HD / 2);
-    const uint8_t* ks = a.ks + first * (HD / kMxBlock);
+    const uint8_t* ks = a.ks + first * CT;
     const uint8_t* vc = a.vc + first * (HD / 2);
-    const uint8_t* vs = a.vs + first * (HD / kMxBlock);
+    const uint8_t* vs = a.vs + first * CT;
 
     floatx16 o[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.f;
-    float m = -INFINITY, l = 0.f;
-    char* vb = vbuf[w];
-    for (int k0 = w * kMxKeys; k0 < len; k0 += kMxAttWaves * kMxKeys) {
-        // V: lane (key, chunk) decodes 32 channels into LDS
+    float m = -INFINITY, l = 0.f;                        // the exponents' reference; l of this lane's keys
+    char* vb = lds + w * kV;
+    KvStep<HD> next;
+    if (s0 + w < s1) next.load(kc, ks, vc, vs, (s0 + w) * kMxKeys, len, lane);
+    for (int st = s0 + w; st < s1; st += NW) {
+        const KvStep<HD> cur = next;
+        const int k0 = st * kMxKeys;
+        if (st + NW < s1) next.load(kc, ks, vc, vs, k0 + NW * kMxKeys, len, lane);
+        const bool whole = k0 + kMxKeys <= len;
+        // V: lane (key, chunk) decodes 32 channels into LDS; keys past the end, which
+        // may hold anything, also NaN, as zeros
 #pragma unroll
-        for (int u = 0; u < kMxKeys * CT / kWave; ++u) {
+        for (int u = 0; u < KvStep<HD>::VU; ++u) {
             const int at = u * kWave + lane, key = at / CT, c = at % CT;
-            const bool in = k0 + key < len;
-            const size_t kr = min(k0 + key, len - 1);
-            const uint4 code = ld16(vc + kr * (HD / 2) + 16 * c);
-            const float sc = in ? mx_scale(vs[kr * (HD / kMxBlock) + c]) : 1.f;
-            const uint32_t keep = in ? ~0u : 0u;         // keys past the end hold anything, also NaN
+            uint4 code = cur.v[u];
+            float sc = mx_scale(cur.vs[u]);
+            if (!whole && k0 + key >= len) {
+                code = zero16();
+                sc = 1.f;
+            }
             char* d = vb + key * kPitch + 64 * c;
-            st16(d, mx_fp4_bf16(code.x & keep, sc));
-            st16(d + 16, mx_fp4_bf16(code.y & keep, sc));
-            st16(d + 32, mx_fp4_bf16(code.z & keep, sc));
-            st16(d + 48, mx_fp4_bf16(code.w & keep, sc));
+            st16(d, mx_fp4_bf16(code.x, sc));
+            st16(d + 16, mx_fp4_bf16(code.y, sc));
+            st16(d + 32, mx_fp4_bf16(code.z, sc));
+            st16(d + 48, mx_fp4_bf16(code.w, sc));
         }
         floatx16 s;
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[j] = 0.f;
-        const size_t kr = min(k0 + i, len - 1);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const uint4 code = ld16(kc + kr * (HD / 2) + 16 * (2 * c + h));
-            const float sc = mx_scale(ks[kr * (HD / kMxBlock) + 2 * c + h]);
-            const uint32_t cw[4] = {code.x, code.y, code.z, code.w};
+            const float sc = mx_scale((cur.ks >> (8 * (2 * c + h))) & 255u);
+            const uint32_t cw[4] = {cur.k[c].x, cur.k[c].y, cur.k[c].z, cur.k[c].w};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const uint4 kf = mx_fp4_bf16(cw[t], sc);
@@ -144,30 +186,35 @@ __global__ __launch_bounds__(kMxAttThreads) void mx_attend_kernel(MxAttArgs a) {
                 for (int n = 0; n < NT; ++n) s = Mma32<true>::step(kf, q[c][t][n], s);
             }
         }
-        float top = -INFINITY;
+        if (!whole) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const bool in = k0 + 8 * (j >> 2) + 4 * h + (j & 3) < len;
-            s[j] = in ? s[j] * a.scale2 : -INFINITY;
-            top = fmaxf(top, s[j]);
+            for (int j = 0; j < 16; ++j)
+                if (k0 + mfma32_row(lane, j) >= len) s[j] = -INFINITY;
         }
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float mn = fmaxf(m, top);
-        const float ref = mn == -INFINITY ? 0.f : mn;
-        const float f = fast_exp2(m - ref);
-        m = mn;
-        float sum = 0.f;
+        // The reference moves only when a query's largest score passes it by more than
+        // kMxSlack (exponents stay below 2^8, and (m, l, O) are exact for any
+        // reference), so that O is rarely rescaled.
+        float top = s[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale2;
+        if (__builtin_amdgcn_ballot_w64(top > m + kMxSlack || m == -INFINITY) != 0) {
+            const float mn = fmaxf(m, top);
+            const float f = fast_exp2(m - (mn == -INFINITY ? 0.f : mn));
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[c][j] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
         float p[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            p[j] = fast_exp2(s[j] - ref);
-            sum += p[j];
+            p[j] = fast_exp2(fmaf(s[j], a.scale2, -ref));
+            l += p[j];
         }
-        l = l * f + sum;                                 // of this lane's keys
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[c][j] *= f;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             uint4 pt[NT];
@@ -175,15 +222,16 @@ __global__ __launch_bounds__(kMxAttThreads) void mx_attend_kernel(MxAttArgs a) {
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 // channel 32 c + i; keys 16 u + 4 h + 0..3 and 8 further on, as p's registers
-                const char* s0 = vb + (16 * u + 4 * h + ((lane & 15) >> 2)) * kPitch + 64 * c +
-                                 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-                const uint2 v0 = lds_read_tr(s0), v1 = lds_read_tr(s0 + 8 * kPitch);
-                const uint4 vf = make_uint4(v0.x, v0.y, v1.x, v1.y);
+                const char* v0 = vb + (16 * u + 4 * h + ((lane & 15) >> 2)) * kPitch + 64 * c + 32 * ((lane >> 4) & 1) +
+                                 8 * (lane & 3);
+                const uint2 x = lds_read_tr(v0), y = lds_read_tr(v0 + 8 * kPitch);
+                const uint4 vf = make_uint4(x.x, x.y, y.x, y.y);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) o[c] = Mma32<true>::step(vf, pt[n], o[c]);
             }
         }
     }
+    // the waves' parts: to the common reference, then added in pairs
     l += __shfl_xor(l, 32);
     if (h == 0) {
         sm[w][i] = m;
@@ -192,52 +240,138 @@ __global__ __launch_bounds__(kMxAttThreads) void mx_attend_kernel(MxAttArgs a) {
     __syncthreads();
     float mt = -INFINITY, lt = 0.f;
 #pragma unroll
-    for (int x = 0; x < kMxAttWaves; ++x) mt = fmaxf(mt, sm[x][i]);
+    for (int x = 0; x < NW; ++x) mt = fmaxf(mt, sm[x][i]);
     const float ref = mt == -INFINITY ? 0.f : mt;
 #pragma unroll
-    for (int x = 0; x < kMxAttWaves; ++x) lt += sl[x][i] * fast_exp2(sm[x][i] - ref);
-    const float f = fast_exp2(m - ref);
-    // the waves' O, one after another
-    for (int x = 0; x < kMxAttWaves; ++x) {
-        if (x == w) {
+    for (int x = 0; x < NW; ++x) lt += sl[x][i] * fast_exp2(sm[x][i] - ref);
+    // l counts the keys, so it is 0 only where there were none (zeros) or where no
+    // score is finite (NaN, as the quotient)
+    const float f = fast_exp2(m - ref) * (a.splits > 1 ? 1.f : len > 0 ? 1.f / lt : 0.f);
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
+    for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float4* d = reinterpret_cast<float4*>(&so[i][32 * c + 8 * j + 4 * h]);
-                    float4 v = make_float4(o[c][4 * j] * f, o[c][4 * j + 1] * f, o[c][4 * j + 2] * f, o[c][4 * j + 3] * f);
-                    if (x > 0) {
-                        const float4 e = *d;
-                        v = make_float4(v.x + e.x, v.y + e.y, v.z + e.z, v.w + e.w);
-                    }
-                    *d = v;
-                }
-        }
+        for (int j = 0; j < 16; ++j) o[c][j] *= f;
+    auto each = [&](int buf, auto fn) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                fn(reinterpret_cast<float4*>(lds + buf * kO + i * kOPitch + (32 * c + 8 * j + 4 * h) * 4), c, 4 * j);
+    };
+    auto put = [&](float4* d, int c, int j) { *d = make_float4(o[c][j], o[c][j + 1], o[c][j + 2], o[c][j + 3]); };
+#pragma unroll
+    for (int half = NW / 2; half >= 1; half /= 2) {
+        if (w >= half && w < 2 * half) each(w - half, put);
+        __syncthreads();
+        if (w < half)
+            each(w, [&](const float4* d, int c, int j) {
+                const float4 v = *d;
+                o[c][j] += v.x; o[c][j + 1] += v.y; o[c][j + 2] += v.z; o[c][j + 3] += v.w;
+            });
         __syncthreads();
     }
-    // an empty sequence: zeros
-    if (threadIdx.x < kMxQ && qv < nq && a.lse)
-        a.lse[(static_cast<size_t>(b) * a.heads + head) * a.n_rows + row] = (mt + __log2f(lt)) * kLn2;
-    for (int x = threadIdx.x; x < kMxQ * HD / 8; x += kMxAttThreads) {
+    if (w == 0) each(0, put);
+    __syncthreads();
+    const size_t slot = ((static_cast<size_t>(b) * a.kv_heads + g) * a.splits + split) * nq;
+    if (threadIdx.x < kMxQ && qv < nq) {
+        if (a.splits > 1) a.ml[slot + qv] = make_float2(mt, lt);
+        else if (a.lse) a.lse[(static_cast<size_t>(b) * a.heads + head) * a.n_rows + row] = (mt + __log2f(lt)) * kLn2;
+    }
+    for (int x = threadIdx.x; x < kMxQ * HD / 8; x += NW * kWave) {
         const int r = x / (HD / 8), c = (x % (HD / 8)) * 8;
         const int qx = qt * kMxQ + r;
         if (qx >= nq) continue;
-        float lq = 0.f, mq = -INFINITY;
-        for (int y = 0; y < kMxAttWaves; ++y) mq = fmaxf(mq, sm[y][r]);
-        const float rq = mq == -INFINITY ? 0.f : mq;
-        for (int y = 0; y < kMxAttWaves; ++y) lq += sl[y][r] * fast_exp2(sm[y][r] - rq);
-        const float inv = len > 0 ? 1.f / lq : 0.f;
-        const size_t at = ((static_cast<size_t>(b) * a.n_rows + qx % a.n_rows) * a.heads + g * group + qx / a.n_rows) * HD + c;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = len > 0 ? so[r][c + e] * inv : 0.f;
-        if constexpr (BF16) {
-            st16(a.out + 2 * at, make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
-                                            pack_bf16x2(v[6], v[7])));
-        } else {
-            *reinterpret_cast<float4*>(a.out + 4 * at) = make_float4(v[0], v[1], v[2], v[3]);
-            *reinterpret_cast<float4*>(a.out + 4 * at + 16) = make_float4(v[4], v[5], v[6], v[7]);
+        const float4* s = reinterpret_cast<const float4*>(lds + r * kOPitch + 4 * c);
+        const float4 u = s[0], v = s[1];
+        if (a.splits > 1) {
+            float4* d = reinterpret_cast<float4*>(a.part + (slot + qx) * HD + c);
+            d[0] = u;
+            d[1] = v;
+            continue;
         }
+        const size_t at = ((static_cast<size_t>(b) * a.n_rows + qx % a.n_rows) * a.heads + g * group + qx / a.n_rows) * HD + c;
+        if constexpr (BF16) {
+            st16(a.out + 2 * at, make_uint4(pack_bf16x2(u.x, u.y), pack_bf16x2(u.z, u.w), pack_bf16x2(v.x, v.y),
+                                            pack_bf16x2(v.z, v.w)));
+        } else {
+            *reinterpret_cast<float4*>(a.out + 4 * at) = u;
+            *reinterpret_cast<float4*>(a.out + 4 * at + 16) = v;
+        }
+    }
+}
+
+// The splits' parts of a query vector, a wave each: lane s weighs split s, then
+// every lane adds its channels over the splits.  grid (queries / 4, kv_heads, batch)
+template <bool BF16, int HD>
+__global__ __launch_bounds__(256) void mx_attend_merge_kernel(MxAttArgs a) {
+    constexpr int ES = Elem<BF16>::kBytes, CH = HD / kWave;
+    const int lane = threadIdx.x & 63;
+    const int group = a.heads / a.kv_heads, nq = group * a.n_rows;
+    const int qv = blockIdx.x * 4 + (threadIdx.x >> 6), g = blockIdx.y, b = blockIdx.z;
+    if (qv >= nq) return;
+    const size_t slot = (static_cast<size_t>(b) * a.kv_heads + g) * a.splits * nq + qv;
+    float2 e = make_float2(-INFINITY, 0.f);
+    if (lane < a.splits) e = a.ml[slot + static_cast<size_t>(lane) * nq];
+    const float m = wave_max(e.x);
+    const float wgt = fast_exp2(e.x - (m == -INFINITY ? 0.f : m));
+    const float l = wave_sum(e.y * wgt);
+    float v[CH] = {};
+    for (int s = 0; s < a.splits; ++s) {
+        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wgt), s));
+        const float* p = a.part + (slot + static_cast<size_t>(s) * nq) * HD + lane * CH;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] = fmaf(p[c], ws, v[c]);
+    }
+    const bool any = a.kv_len == nullptr || a.kv_len[b] > 0;
+    const int head = g * group + qv / a.n_rows, row = qv % a.n_rows;
+    char* d = a.out + (((static_cast<size_t>(b) * a.n_rows + row) * a.heads + head) * HD + lane * CH) * ES;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) v[c] = any ? v[c] / l : 0.f;
+    if constexpr (BF16 && CH == 2) *reinterpret_cast<uint32_t*>(d) = pack_bf16x2(v[0], v[1]);
+    else if constexpr (BF16) *reinterpret_cast<uint16_t*>(d) = static_cast<uint16_t>(f32_to_bf16_bits(v[0]));
+    else
+#pragma unroll
+        for (int c = 0; c < CH; ++c) reinterpret_cast<float*>(d)[c] = v[c];
+    if (a.lse && lane == 0) a.lse[(static_cast<size_t>(b) * a.heads + head) * a.n_rows + row] = (m + __log2f(l)) * kLn2;
+}
+
+// Waves per workgroup and key splits: eight waves where the workgroups are fewer
+// than the compute units, and as many splits as bring two waves to each SIMD,
+// while a wave has two steps or more.
+struct MxAttPlan {
+    int tiles, waves, splits;
+    size_t part, total;                                  // bytes: O parts, with the sums
+};
+MxAttPlan mx_att_plan(int batch, int seq, int heads, int kv_heads, int hd, int n_rows) {
+    MxAttPlan p{};
+    const long nq = static_cast<long>(heads / kv_heads) * n_rows;
+    p.tiles = ceil_div(nq, kMxQ);
+    const long wgs = static_cast<long>(batch) * kv_heads * p.tiles;
+    const int steps = ceil_div(seq, kMxKeys);
+    p.waves = steps >= 16 && wgs <= 256 ? 8 : 4;
+    long splits = (2048 + wgs * p.waves - 1) / (wgs * p.waves);
+    const long most = steps / (2 * p.waves);
+    if (splits > most) splits = most;
+    if (splits > kMxMaxSplits) splits = kMxMaxSplits;
+    p.splits = splits < 1 ? 1 : static_cast<int>(splits);
+    if (p.splits > 1) {
+        const size_t rows = static_cast<size_t>(batch) * kv_heads * p.splits * nq;
+        p.part = align_up(rows * hd * sizeof(float), 256);
+        p.total = p.part + rows * sizeof(float2);
+    }
+    return p;
+}
+
+template <bool BF16, int HD>
+void mx_att_launch(const MxAttPlan& p, const MxAttArgs& a, int batch, hipStream_t stream) {
+    const dim3 grid(p.tiles * a.kv_heads, p.splits, batch);
+    if (p.waves == 8)
+        hipLaunchKernelGGL((mx_attend_kernel<BF16, HD, 8>), grid, dim3(8 * kWave), 0, stream, a);
+    else
+        hipLaunchKernelGGL((mx_attend_kernel<BF16, HD, 4>), grid, dim3(4 * kWave), 0, stream, a);
+    if (p.splits > 1) {
+        const dim3 merge(ceil_div(static_cast<long>(a.heads / a.kv_heads) * a.n_rows, 4), a.kv_heads, batch);
+        hipLaunchKernelGGL((mx_attend_merge_kernel<BF16, HD>), merge, dim3(256), 0, stream, a);
     }
 }
 
@@ -247,7 +381,10 @@ __global__ __launch_bounds__(kMxAttThreads) void mx_attend_kernel(MxAttArgs a) {
 extern "C" size_t polestar_mx_attend_workspace_size(polestar_dtype dtype, int batch, int seq, int n_heads,
                                                     int n_kv_heads, int head_dim, int n_rows) {
     using namespace ps;
-    return 0;
+    if (!dtype_ok(dtype) || batch <= 0 || seq <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_rows <= 0 ||
+        n_heads % n_kv_heads != 0 || (head_dim != 64 && head_dim != 128))
+        return 0;
+    return mx_att_plan(batch, seq, n_heads, n_kv_heads, head_dim, n_rows).total;
 }
 
 extern "C" polestar_status polestar_mx_attend(polestar_dtype dtype, int batch, int seq, int n_heads, int n_kv_heads,
@@ -262,21 +399,24 @@ extern "C" polestar_status polestar_mx_attend(polestar_dtype dtype, int batch, i
         !v_codes || !v_scales || !out)
         return POLESTAR_ERR_INVALID_ARGUMENT;
     const long nq = static_cast<long>(n_heads / n_kv_heads) * n_rows;
-    const long tiles = (nq + kMxQ - 1) / kMxQ;
     if ((head_dim != 64 && head_dim != 128) || !row_ok(dtype, q_stride) || !aligned16(q) || !aligned16(k_codes) ||
         !aligned16(v_codes) || !aligned_to(k_scales, head_dim / kMxBlock) || !aligned_to(v_scales, head_dim / kMxBlock) ||
-        !aligned16(out) || !aligned16(workspace) || batch > 65535 || tiles * n_kv_heads > 0xffffff)
+        !aligned16(out) || !aligned16(workspace) || batch > 65535 || n_kv_heads > 65535 ||
+        (nq + kMxQ) / kMxQ * n_kv_heads > 0x7fffff || seq > 0x7fffffff - 1024)
         return POLESTAR_ERR_UNSUPPORTED;
-    const size_t need = polestar_mx_attend_workspace_size(dtype, batch, seq, n_heads, n_kv_heads, head_dim, n_rows);
-    if (workspace_bytes < need || (need > 0 && !workspace)) return POLESTAR_ERR_WORKSPACE;
+    const MxAttPlan p = mx_att_plan(batch, seq, n_heads, n_kv_heads, head_dim, n_rows);
+    if (workspace_bytes < p.total || (p.total > 0 && !workspace)) return POLESTAR_ERR_WORKSPACE;
     if (!(scale > 0.f)) scale = 1.f / sqrtf(static_cast<float>(head_dim));
     const MxAttArgs a{static_cast<const char*>(q), q_stride, k_codes, k_scales, v_codes, v_scales, kv_len,
-                      static_cast<char*>(out), lse, scale * kLog2e, seq, n_rows, n_heads, n_kv_heads,
-                      static_cast<int>(tiles)};
-    const dim3 grid(static_cast<unsigned>(tiles * n_kv_heads), batch);
-#define PS_ATT(BF, HD) hipLaunchKernelGGL((mx_attend_kernel<BF, HD>), grid, dim3(kMxAttThreads), 0, stream, a)
-    if (dtype == POLESTAR_BF16) { if (head_dim == 128) PS_ATT(true, 128); else PS_ATT(true, 64); }
-    else { if (head_dim == 128) PS_ATT(false, 128); else PS_ATT(false, 64); }
-#undef PS_ATT
+                      static_cast<char*>(out), lse, scale * kLog2e, seq, n_rows, n_heads, n_kv_heads, p.tiles, p.splits,
+                      static_cast<float*>(workspace),
+                      reinterpret_cast<float2*>(static_cast<char*>(workspace) + p.part)};
+    if (dtype == POLESTAR_BF16) {
+        if (head_dim == 128) mx_att_launch<true, 128>(p, a, batch, stream);
+        else mx_att_launch<true, 64>(p, a, batch, stream);
+    } else {
+        if (head_dim == 128) mx_att_launch<false, 128>(p, a, batch, stream);
+        else mx_att_launch<false, 64>(p, a, batch, stream);
+    }
     return launch_status();
 }
