@@ -24,6 +24,7 @@ namespace {
 constexpr int kMxKeys = 32;                              // keys of a wave's step
 constexpr int kMxQ = 32;                                 // query vectors of a workgroup
 constexpr int kMxMaxSplits = 64;                         // a lane each in the merge
+constexpr int kMxMaxSeq = 1 << 24;                       // a head's codes: offsets of 32 bits
 constexpr float kMxSlack = 8.f;                          // see the softmax
 
 typedef short shortx4 __attribute__((ext_vector_type(4)));
@@ -68,29 +69,48 @@ __device__ __forceinline__ void split_bf16(const float* v, uint4* o) {
     }
 }
 
+// V's rows in LDS: 2 HD bytes of a key and 64 more, and within each 64 bytes (the
+// 32 channels that a lane decodes) the 16-byte chunks XORed by v_swizzle(key), so
+// that the lanes whose stores run together, and the eight rows of a transposed
+// read, lie in different banks.  (Without it half of the LDS cycles were conflicts.)
+template <int HD> __device__ __forceinline__ int v_swizzle(int key) { return (HD == 128 ? key : key ^ (key >> 2)) & 3; }
+
+// A head's keys or values: buffers that end with the sequence's last key, so that
+// what lies behind it (which may hold anything) reads as 0.
+typedef __amdgpu_buffer_rsrc_t KvBuffer;
+__device__ __forceinline__ KvBuffer kv_buffer(const uint8_t* base, size_t off, uint32_t bytes) {
+    const uint64_t p = reinterpret_cast<uint64_t>(base) + off;
+    const uint64_t u = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p >> 32))) << 32 |
+                       static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(p)));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(u), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
+}
+
 // The codes of a step's 32 keys: lane (key i, half h) holds half of key i's, and of
 // V's rows the chunks that it will decode.
 template <int HD> struct KvStep {
-    static constexpr int NC = HD / 64, VU = HD / 64;
+    static constexpr int CT = HD / 32, NC = HD / 64, VU = HD / 64;
     uint4 k[NC], v[VU];
     uint32_t ks, vs[VU];
-    __device__ __forceinline__ void load(const uint8_t* kc, const uint8_t* kss, const uint8_t* vc, const uint8_t* vss,
-                                         int k0, int len, int lane) {
-        constexpr int CT = HD / 32;
-        const size_t kr = min(k0 + (lane & 31), len - 1);
+    __device__ __forceinline__ void load(KvBuffer kc, KvBuffer kss, KvBuffer vc, KvBuffer vss, int k0, int lane) {
+        const int i = lane & 31, h = lane >> 5;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) k[c] = ld16(kc + kr * (HD / 2) + 16 * (2 * c + (lane >> 5)));
-        if constexpr (HD == 128) ks = reinterpret_cast<const uint32_t*>(kss)[kr];
-        else ks = reinterpret_cast<const uint16_t*>(kss)[kr];
+        for (int c = 0; c < NC; ++c)
+            k[c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(kc, i * (HD / 2) + 16 * h, k0 * (HD / 2) + 32 * c, 0));
+        if constexpr (HD == 128) ks = __builtin_amdgcn_raw_buffer_load_b32(kss, i * CT, k0 * CT, 0);
+        else ks = __builtin_amdgcn_raw_buffer_load_b16(kss, i * CT, k0 * CT, 0);
 #pragma unroll
         for (int u = 0; u < VU; ++u) {
-            const int at = u * kWave + lane;
-            const size_t vr = min(k0 + at / CT, len - 1);
-            v[u] = ld16(vc + vr * (HD / 2) + 16 * (at % CT));
-            vs[u] = vss[vr * CT + at % CT];
+            v[u] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(vc, 16 * lane, k0 * (HD / 2) + 16 * kWave * u, 0));
+            vs[u] = __builtin_amdgcn_raw_buffer_load_b8(vss, lane, k0 * CT + kWave * u, 0);
         }
     }
 };
+
+// The larger of a lane's value and that of the lane 32 away.
+__device__ __forceinline__ float max_halves(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
 // grid (tiles * kv_heads, splits, batch), NW waves
 template <bool BF16, int HD, int NW>
@@ -105,7 +125,7 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
     __shared__ __align__(16) char lds[NW * kV > NW / 2 * kO ? NW * kV : NW / 2 * kO];
     __shared__ float sm[NW][kMxQ], sl[NW][kMxQ];
 
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 31, h = lane >> 5;
     const int b = blockIdx.z, g = blockIdx.x / a.tiles, qt = blockIdx.x % a.tiles, split = blockIdx.y;
     const int group = a.heads / a.kv_heads;
@@ -117,6 +137,12 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
     // this split's steps, of the sequence's own length
     const int steps = (len + kMxKeys - 1) / kMxKeys, per = (steps + a.splits - 1) / a.splits;
     const int s0 = min(split * per, steps), s1 = min(s0 + per, steps);
+
+    const size_t first = (static_cast<size_t>(b) * a.kv_heads + g) * a.seq;   // the head's first key
+    const KvBuffer kc = kv_buffer(a.kc, first * (HD / 2), len * (HD / 2)), ks = kv_buffer(a.ks, first * CT, len * CT);
+    const KvBuffer vc = kv_buffer(a.vc, first * (HD / 2), len * (HD / 2)), vs = kv_buffer(a.vs, first * CT, len * CT);
+    KvStep<HD> even, odd;                                // this step's codes and the next one's, in turn
+    even.load(kc, ks, vc, vs, (s0 + w) * kMxKeys, lane);
 
     uint4 q[NC][4][NT];
     {
@@ -135,12 +161,6 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
                 }
             }
     }
-    const size_t first = (static_cast<size_t>(b) * a.kv_heads + g) * a.seq;   // the head's first key
-    const uint8_t* kc = a.kc + first * (HD / 2);
-    const uint8_t* ks = a.ks + first * CT;
-    const uint8_t* vc = a.vc + first * (HD / 2);
-    const uint8_t* vs = a.vs + first * CT;
-
     floatx16 o[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
@@ -148,29 +168,24 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
         for (int j = 0; j < 16; ++j) o[c][j] = 0.f;
     float m = -INFINITY, l = 0.f;                        // the exponents' reference; l of this lane's keys
     char* vb = lds + w * kV;
-    KvStep<HD> next;
-    if (s0 + w < s1) next.load(kc, ks, vc, vs, (s0 + w) * kMxKeys, len, lane);
-    for (int st = s0 + w; st < s1; st += NW) {
-        const KvStep<HD> cur = next;
+    // transposed reads: keys 4 h + 0..3 and 8 further on
+    const int tk = 4 * h + ((lane & 15) >> 2), tq = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    const int tr0 = tk * kPitch + 16 * (tq ^ v_swizzle<HD>(tk)) + 8 * (lane & 1);
+    const int tr1 = (tk + 8) * kPitch + 16 * (tq ^ v_swizzle<HD>(tk + 8)) + 8 * (lane & 1);
+    auto step = [&](int st, const KvStep<HD>& cur) {
         const int k0 = st * kMxKeys;
-        if (st + NW < s1) next.load(kc, ks, vc, vs, k0 + NW * kMxKeys, len, lane);
-        const bool whole = k0 + kMxKeys <= len;
-        // V: lane (key, chunk) decodes 32 channels into LDS; keys past the end, which
-        // may hold anything, also NaN, as zeros
+        // V: lane (key, chunk) decodes 32 channels into LDS
 #pragma unroll
         for (int u = 0; u < KvStep<HD>::VU; ++u) {
             const int at = u * kWave + lane, key = at / CT, c = at % CT;
-            uint4 code = cur.v[u];
-            float sc = mx_scale(cur.vs[u]);
-            if (!whole && k0 + key >= len) {
-                code = zero16();
-                sc = 1.f;
-            }
+            const uint4 code = cur.v[u];
+            const float sc = mx_scale(cur.vs[u]);
             char* d = vb + key * kPitch + 64 * c;
-            st16(d, mx_fp4_bf16(code.x, sc));
-            st16(d + 16, mx_fp4_bf16(code.y, sc));
-            st16(d + 32, mx_fp4_bf16(code.z, sc));
-            st16(d + 48, mx_fp4_bf16(code.w, sc));
+            const int z = 16 * v_swizzle<HD>(key);
+            st16(d + z, mx_fp4_bf16(code.x, sc));
+            st16(d + (z ^ 16), mx_fp4_bf16(code.y, sc));
+            st16(d + (z ^ 32), mx_fp4_bf16(code.z, sc));
+            st16(d + (z ^ 48), mx_fp4_bf16(code.w, sc));
         }
         floatx16 s;
 #pragma unroll
@@ -186,7 +201,7 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
                 for (int n = 0; n < NT; ++n) s = Mma32<true>::step(kf, q[c][t][n], s);
             }
         }
-        if (!whole) {
+        if (k0 + kMxKeys > len) {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 if (k0 + mfma32_row(lane, j) >= len) s[j] = -INFINITY;
@@ -197,7 +212,7 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
         float top = s[0];
 #pragma unroll
         for (int j = 1; j < 16; ++j) top = fmaxf(top, s[j]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale2;
+        top = max_halves(top) * a.scale2;
         if (__builtin_amdgcn_ballot_w64(top > m + kMxSlack || m == -INFINITY) != 0) {
             const float mn = fmaxf(m, top);
             const float f = fast_exp2(m - (mn == -INFINITY ? 0.f : mn));
@@ -222,14 +237,23 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 // channel 32 c + i; keys 16 u + 4 h + 0..3 and 8 further on, as p's registers
-                const char* v0 = vb + (16 * u + 4 * h + ((lane & 15) >> 2)) * kPitch + 64 * c + 32 * ((lane >> 4) & 1) +
-                                 8 * (lane & 3);
-                const uint2 x = lds_read_tr(v0), y = lds_read_tr(v0 + 8 * kPitch);
+                const uint2 x = lds_read_tr(vb + tr0 + 16 * u * kPitch + 64 * c);
+                const uint2 y = lds_read_tr(vb + tr1 + 16 * u * kPitch + 64 * c);
                 const uint4 vf = make_uint4(x.x, x.y, y.x, y.y);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) o[c] = Mma32<true>::step(vf, pt[n], o[c]);
             }
         }
+    };
+    // (the queries' loads end here: inside the loop the wait for them would be one
+    // for the next step's codes)
+    __builtin_amdgcn_s_waitcnt(0);
+    for (int st = s0 + w; st < s1; st += 2 * NW) {
+        odd.load(kc, ks, vc, vs, (st + NW) * kMxKeys, lane);
+        step(st, even);
+        if (st + NW >= s1) break;
+        even.load(kc, ks, vc, vs, (st + 2 * NW) * kMxKeys, lane);
+        step(st + NW, odd);
     }
     // the waves' parts: to the common reference, then added in pairs
     l += __shfl_xor(l, 32);
@@ -300,27 +324,47 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
     }
 }
 
-// The splits' parts of a query vector, a wave each: lane s weighs split s, then
-// every lane adds its channels over the splits.  grid (queries / 4, kv_heads, batch)
-template <bool BF16, int HD>
-__global__ __launch_bounds__(256) void mx_attend_merge_kernel(MxAttArgs a) {
+// The splits' parts of a query vector: lane s weighs split s, then every wave adds
+// its share of the splits, all of its loads in flight (one after another, they took
+// 10 us for 32 splits).  grid (queries, kv_heads, batch), NW waves
+template <bool BF16, int HD, int NW>
+__global__ __launch_bounds__(NW * kWave) void mx_attend_merge_kernel(MxAttArgs a) {
     constexpr int ES = Elem<BF16>::kBytes, CH = HD / kWave;
-    const int lane = threadIdx.x & 63;
+    constexpr int U = kMxMaxSplits / 4 / (NW == 1 ? 2 : 1);   // splits of a wave: NW = 1 takes up to 8
+    __shared__ float red[NW][HD];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int group = a.heads / a.kv_heads, nq = group * a.n_rows;
-    const int qv = blockIdx.x * 4 + (threadIdx.x >> 6), g = blockIdx.y, b = blockIdx.z;
-    if (qv >= nq) return;
+    const int qv = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
     const size_t slot = (static_cast<size_t>(b) * a.kv_heads + g) * a.splits * nq + qv;
     float2 e = make_float2(-INFINITY, 0.f);
     if (lane < a.splits) e = a.ml[slot + static_cast<size_t>(lane) * nq];
+    float p[U][CH];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int s = w + u * NW;
+        const float* src = a.part + (slot + static_cast<size_t>(s) * nq) * HD + lane * CH;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) p[u][c] = s < a.splits ? src[c] : 0.f;
+    }
     const float m = wave_max(e.x);
     const float wgt = fast_exp2(e.x - (m == -INFINITY ? 0.f : m));
     const float l = wave_sum(e.y * wgt);
     float v[CH] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wgt), s));
-        const float* p = a.part + (slot + static_cast<size_t>(s) * nq) * HD + lane * CH;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) v[c] = fmaf(p[c], ws, v[c]);
+    for (int u = 0; u < U; ++u) {
+        const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wgt), w + u * NW));
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] = fmaf(p[u][c], ws, v[c]);
+    }
+    if constexpr (NW > 1) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) red[w][lane * CH + c] = v[c];
+        __syncthreads();
+        if (w > 0) return;
+#pragma unroll
+        for (int x = 1; x < NW; ++x)
+#pragma unroll
+            for (int c = 0; c < CH; ++c) v[c] += red[x][lane * CH + c];
     }
     const bool any = a.kv_len == nullptr || a.kv_len[b] > 0;
     const int head = g * group + qv / a.n_rows, row = qv % a.n_rows;
@@ -335,9 +379,9 @@ __global__ __launch_bounds__(256) void mx_attend_merge_kernel(MxAttArgs a) {
     if (a.lse && lane == 0) a.lse[(static_cast<size_t>(b) * a.heads + head) * a.n_rows + row] = (m + __log2f(l)) * kLn2;
 }
 
-// Waves per workgroup and key splits: eight waves where the workgroups are fewer
-// than the compute units, and as many splits as bring two waves to each SIMD,
-// while a wave has two steps or more.
+// Waves per workgroup and key splits: eight waves where the workgroups are at most
+// the compute units (two waves on each SIMD, which the registers allow), and as
+// many splits as fill them, while a wave has two steps or more.
 struct MxAttPlan {
     int tiles, waves, splits;
     size_t part, total;                                  // bytes: O parts, with the sums
@@ -349,7 +393,7 @@ MxAttPlan mx_att_plan(int batch, int seq, int heads, int kv_heads, int hd, int n
     const long wgs = static_cast<long>(batch) * kv_heads * p.tiles;
     const int steps = ceil_div(seq, kMxKeys);
     p.waves = steps >= 16 && wgs <= 256 ? 8 : 4;
-    long splits = (2048 + wgs * p.waves - 1) / (wgs * p.waves);
+    long splits = (p.waves == 8 ? 256 : 512) / wgs;
     const long most = steps / (2 * p.waves);
     if (splits > most) splits = most;
     if (splits > kMxMaxSplits) splits = kMxMaxSplits;
@@ -370,8 +414,9 @@ void mx_att_launch(const MxAttPlan& p, const MxAttArgs& a, int batch, hipStream_
     else
         hipLaunchKernelGGL((mx_attend_kernel<BF16, HD, 4>), grid, dim3(4 * kWave), 0, stream, a);
     if (p.splits > 1) {
-        const dim3 merge(ceil_div(static_cast<long>(a.heads / a.kv_heads) * a.n_rows, 4), a.kv_heads, batch);
-        hipLaunchKernelGGL((mx_attend_merge_kernel<BF16, HD>), merge, dim3(256), 0, stream, a);
+        const dim3 merge((a.heads / a.kv_heads) * a.n_rows, a.kv_heads, batch);
+        if (p.splits <= 8) hipLaunchKernelGGL((mx_attend_merge_kernel<BF16, HD, 1>), merge, dim3(kWave), 0, stream, a);
+        else hipLaunchKernelGGL((mx_attend_merge_kernel<BF16, HD, 4>), merge, dim3(4 * kWave), 0, stream, a);
     }
 }
 
@@ -402,7 +447,7 @@ extern "C" polestar_status polestar_mx_attend(polestar_dtype dtype, int batch, i
     if ((head_dim != 64 && head_dim != 128) || !row_ok(dtype, q_stride) || !aligned16(q) || !aligned16(k_codes) ||
         !aligned16(v_codes) || !aligned_to(k_scales, head_dim / kMxBlock) || !aligned_to(v_scales, head_dim / kMxBlock) ||
         !aligned16(out) || !aligned16(workspace) || batch > 65535 || n_kv_heads > 65535 ||
-        (nq + kMxQ) / kMxQ * n_kv_heads > 0x7fffff || seq > 0x7fffffff - 1024)
+        (nq + kMxQ) / kMxQ * n_kv_heads > 0x7fffff || seq > kMxMaxSeq)
         return POLESTAR_ERR_UNSUPPORTED;
     const MxAttPlan p = mx_att_plan(batch, seq, n_heads, n_kv_heads, head_dim, n_rows);
     if (workspace_bytes < p.total || (p.total > 0 && !workspace)) return POLESTAR_ERR_WORKSPACE;
