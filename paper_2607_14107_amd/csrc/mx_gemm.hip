@@ -374,6 +374,204 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     }
 }
 
+// ---------------------------------------------------------------------------
+// Few rows: bound by the weights' stream and, below a few MB, by latency.  16 MT
+// rows x 16 NT outputs per workgroup; its waves take chunks of 512 channels in turn
+// (256 bytes of a weight row, 16 of its scales), every load of a chunk issued before
+// its first product, and their sums are added in LDS: no split and no second launch.
+//
+// RAW: the rows come as dtype and are quantized here, a lane the block that it holds
+// (32 channels: no exchange for the maximum), so that one launch does both; every
+// workgroup repeats that work, which is why only 16 rows are taken this way.
+// ---------------------------------------------------------------------------
+
+constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave;
+constexpr int kFewRows = 64;                             // most rows of these kernels
+
+struct MxFewArgs : MxGemmArgs {
+    const char* raw;                                     // [batch][seq][n_in] dtype
+    int seq, row_start, n_rows;
+};
+
+// Buffers whose end is checked, for loads into registers.
+typedef __amdgpu_buffer_rsrc_t MxRows;
+__device__ __forceinline__ MxRows mx_rows(const uint8_t* base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, bytes, 0x00027000);
+}
+__device__ __forceinline__ uint4 mx_load16(MxRows b, uint32_t lane_off, uint32_t off) {
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b, lane_off, off, 0));
+}
+
+// The operand of a step, 128 channels from LDS-free loads.  MXFP8 codes: as
+// Frag<MXFP8>'s loads, from memory.
+constexpr uint32_t kMxPastEnd = 0x40000000u;             // an offset behind every such buffer: reads as 0
+template <int FMT, bool DEC>
+__device__ __forceinline__ void frag_load(Frag<FMT, DEC>& f, MxRows b, uint32_t row, uint32_t step, bool in, int g) {
+    if constexpr (FMT == POLESTAR_MXFP4) {
+        f.c = mx_load16(b, row + 16 * g, in ? 64 * step : kMxPastEnd);
+    } else {
+        f.c[0] = mx_load16(b, row + (DEC ? 32 * g : 16 * g), in ? 128 * step : kMxPastEnd);
+        f.c[1] = mx_load16(b, row + (DEC ? 32 * g + 16 : 64 + 16 * g), in ? 128 * step : kMxPastEnd);
+    }
+}
+
+__device__ __forceinline__ void swap_rows16(uint32_t& a, uint32_t& b) {   // a's odd 16 lanes with b's even ones
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+
+// 32 channels of block g quantized to the lane's operand; returns the scale byte of
+// the block that the instruction expects it for.  MXFP8 (not decoded): lanes 0-15 and
+// 16-31 hold the halves of two blocks each, so they exchange them, and the blocks in
+// the instruction's order are 0, 2, 1, 3: the weights' lanes load them in that order.
+template <int FMT, bool DEC>
+__device__ __forceinline__ uint32_t frag_quantize(Frag<FMT, DEC>& f, const float* v) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    uint32_t byte = mx_scale_byte<FMT>(m);
+    const float sc = mx_scale(byte);
+    const uint32_t keep = byte == kMxNanScale ? 0u : ~0u;
+    if constexpr (FMT == POLESTAR_MXFP4) {
+        f.c = make_uint4(mx_pack_fp4(v, sc) & keep, mx_pack_fp4(v + 8, sc) & keep, mx_pack_fp4(v + 16, sc) & keep,
+                         mx_pack_fp4(v + 24, sc) & keep);
+    } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = mx_pack_fp8(v + 4 * i, sc) & keep;
+        if constexpr (!DEC) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) swap_rows16(w[i], w[4 + i]);
+            const int lane = threadIdx.x & 63, g = lane >> 4;
+            byte = __shfl(static_cast<int>(byte), (lane & 15) + 16 * (g == 1 ? 2 : g == 2 ? 1 : g));
+        }
+        f.c[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        f.c[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+    return byte;
+}
+
+template <int FMT, bool BF16, bool RAW, int MT, int NT>
+__global__ __launch_bounds__(kFewThreads) void mx_few_kernel(MxFewArgs g) {
+    constexpr bool DEC = FMT == POLESTAR_MXFP8 && !BF16;
+    constexpr bool kSwap = RAW && FMT == POLESTAR_MXFP8 && !DEC;   // blocks in the order 0, 2, 1, 3
+    constexpr int ES = BF16 ? 2 : 4;
+    constexpr int S = 4;                                 // steps of a chunk
+    static_assert(!RAW || MT == 1, "rows quantized here: one row tile");
+    __shared__ floatx4 red[kFewWaves][MT * NT][kWave];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, grp = lane >> 4;
+    const int wgrp = kSwap ? (grp == 1 ? 2 : grp == 2 ? 1 : grp) : grp;
+    const int n0 = blockIdx.x * 16 * NT, rows = static_cast<int>(g.rows);
+    const uint32_t xrow = static_cast<uint32_t>(g.n_in / 8) * Mx<FMT>::kBits, wrow = g.n_in / 2, srow = g.n_in / 32;
+    const uint32_t nrows = min(g.n_out - n0, 16 * NT);
+    const MxRows wbuf = mx_rows(g.w + static_cast<size_t>(n0) * wrow, nrows * wrow);
+    const MxRows wsbuf = mx_rows(g.ws + static_cast<size_t>(n0) * srow, nrows * srow);
+    const MxRows xbuf = mx_rows(g.x, rows * xrow), xsbuf = mx_rows(g.xs, rows * srow);
+    const char* raw = nullptr;
+    if constexpr (RAW) {
+        const int m = min(r, rows - 1);                  // past the end: the last one, not stored
+        raw = g.raw + (static_cast<size_t>(m / g.n_rows) * g.seq + g.row_start + m % g.n_rows) * g.n_in * ES + 32 * grp * ES;
+    }
+    const int nsteps = g.n_in / 128;
+    floatx4 acc[MT][NT];
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+    // TAIL: steps past the end multiply zeros by finite numbers
+    auto chunk = [&](int c0, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        auto in = [&](int s) { return !TAIL || c0 + s < nsteps; };
+        Frag<POLESTAR_MXFP4, DEC> fw[S][NT];
+        uint4 sw[NT], sx[MT];
+        Frag<FMT, DEC> fx[S][MT];
+        uint4 rv[RAW ? S : 1][RAW ? 2 * ES : 1];
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int b = 0; b < NT; ++b) frag_load(fw[s][b], wbuf, (16 * b + r) * wrow, c0 + s, in(s), wgrp);
+#pragma unroll
+        for (int b = 0; b < NT; ++b) sw[b] = mx_load16(wsbuf, (16 * b + r) * srow, 4 * c0);
+        if constexpr (RAW) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const char* p = raw + static_cast<size_t>(min(c0 + s, nsteps - 1)) * 128 * ES;
+#pragma unroll
+                for (int i = 0; i < 2 * ES; ++i) rv[s][i] = ld16(p + 16 * i);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int a = 0; a < MT; ++a) frag_load(fx[s][a], xbuf, (16 * a + r) * xrow, c0 + s, in(s), grp);
+#pragma unroll
+            for (int a = 0; a < MT; ++a) sx[a] = mx_load16(xsbuf, (16 * a + r) * srow, 4 * c0);
+        }
+        __builtin_amdgcn_sched_barrier(0);               // every load first
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            auto byte_of = [&](const uint4& v, int q) {
+                const uint32_t d = s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w;
+                return in(s) ? (d >> (8 * q)) & 255u : 127u;
+            };
+            uint32_t bx[MT];
+            if constexpr (RAW) {
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 2 * ES; ++i) Elem<BF16>::unpack(rv[s][i], v + i * Elem<BF16>::E);
+                if constexpr (TAIL) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = in(s) ? v[i] : 0.f;
+                }
+                bx[0] = frag_quantize<FMT, DEC>(fx[s][0], v);
+            } else {
+#pragma unroll
+                for (int a = 0; a < MT; ++a) bx[a] = byte_of(sx[a], grp);
+            }
+#pragma unroll
+            for (int b = 0; b < NT; ++b) {
+                const uint32_t bw = byte_of(sw[b], wgrp);
+                uint4 dw[4];
+                if constexpr (DEC) fw[s][b].decode(dw, mx_scale(bw));
+#pragma unroll
+                for (int a = 0; a < MT; ++a) {
+                    if constexpr (DEC) {
+                        uint4 dx[4];
+                        fx[s][a].decode(dx, mx_scale(bx[a]));
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) acc[a][b] = mfma_bf16(dw[t], dx[t], acc[a][b]);
+                    } else {
+                        acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                            fw[s][b].codes(), fx[s][a].codes(), acc[a][b], Mx<POLESTAR_MXFP4>::kMfma, Mx<FMT>::kMfma, 0, bw,
+                            0, bx[a]);
+                    }
+                }
+            }
+        }
+    };
+    int c0 = w * S;
+    for (; c0 + S <= nsteps; c0 += kFewWaves * S) chunk(c0, std::false_type{});
+    if (c0 < nsteps) chunk(c0, std::true_type{});
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b) red[w][a * NT + b][lane] = acc[a][b];
+    __syncthreads();
+    for (int t = threadIdx.x; t < MT * NT * kWave; t += kFewThreads) {
+        const int tile = t / kWave, l = t % kWave;
+        floatx4 v = red[0][tile][l];
+#pragma unroll
+        for (int x = 1; x < kFewWaves; ++x) v += red[x][tile][l];
+        const int m = 16 * (tile / NT) + (l & 15), n = n0 + 16 * (tile % NT) + 4 * (l >> 4);
+        if (m >= rows || n >= g.n_out) continue;
+        const size_t at = static_cast<size_t>(m) * g.n_out + n;
+        if constexpr (BF16) *reinterpret_cast<uint2*>(g.y + 2 * at) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
+        else *reinterpret_cast<floatx4*>(g.y + 4 * at) = v;
+    }
+}
+
 // The splits' partials, added in order; four outputs per thread.
 template <bool BF16>
 __global__ __launch_bounds__(256) void mx_reduce_kernel(const float* __restrict__ part, int ksplit, long n4,
@@ -425,6 +623,36 @@ MxPlan mx_plan(int x_fmt, bool bf16, long rows, int n_out, int n_in) {
     return p;
 }
 
+// (MT, NT) of the few-rows kernels; nt as mx_few_nt gives it.
+template <int FMT, bool BF16>
+void mx_launch_few(const MxFewArgs& g, int nt, hipStream_t stream) {
+    constexpr bool kDec = FMT == POLESTAR_MXFP8 && !BF16;   // no registers for (4, 2)
+    if (kDec && g.rows > 32) nt = 1;
+    const dim3 grid(ceil_div(g.n_out, 16 * nt)), block(kFewThreads);
+#define PS_FEW(RAW, MT, NT) hipLaunchKernelGGL((mx_few_kernel<FMT, BF16, RAW, MT, NT>), grid, block, 0, stream, g)
+    if (g.raw) { if (nt == 1) PS_FEW(true, 1, 1); else PS_FEW(true, 1, 2); }
+    else if (g.rows <= 16) { if (nt == 1) PS_FEW(false, 1, 1); else PS_FEW(false, 1, 2); }
+    else if (g.rows <= 32) { if (nt == 1) PS_FEW(false, 2, 1); else PS_FEW(false, 2, 2); }
+    else if constexpr (!kDec) { if (nt == 1) PS_FEW(false, 4, 1); else PS_FEW(false, 4, 2); }
+    else PS_FEW(false, 4, 1);
+#undef PS_FEW
+}
+
+// Output tiles of a few-rows workgroup: two where one would make more than two
+// workgroups per compute unit.
+int mx_few_nt(int n_out) { return ceil_div(n_out, 16) > 2 * kMxCus ? 2 : 1; }
+
+// Whether the few-rows kernels take a product: where the rows' codes, which every
+// workgroup reads again, are at most 34 MB in all.  Against the tile kernel's best
+// plan, us: 4096 x 4096, MXFP8, 1 row 3.5 (7.1), 16 rows (17 MB) 5.1 (7.7), 32 rows
+// (34 MB) 7.2 (8.7), 64 rows (67 MB) 11.3 (10.3); 12288 x 4096, 1 row (2 MB) 8.3
+// (9.8), 16 rows (25 MB) 11.1 (10.5), 32 rows (50 MB) 16.2 (11.7).
+bool mx_few(int x_fmt, long rows, int n_out, int n_in) {
+    if (rows > kFewRows) return false;
+    const long read = rows <= 16 ? rows : rows <= 32 ? 32 : 64;
+    return read * polestar_codec_row_bytes(x_fmt, n_in) * ceil_div(n_out, 16 * mx_few_nt(n_out)) <= 34L << 20;
+}
+
 template <int FMT, bool BF16>
 void mx_launch(const MxPlan& p, const MxGemmArgs& g, hipStream_t stream) {
     const dim3 grid(g.row_tiles * g.col_tiles * g.ksplit), block(kMxTileThreads);
@@ -446,11 +674,28 @@ void mx_launch(const MxPlan& p, const MxGemmArgs& g, hipStream_t stream) {
 bool mx_fmt_ok(int fmt) { return fmt == POLESTAR_MXFP4 || fmt == POLESTAR_MXFP8; }
 
 size_t mx_linear_ws(int x_fmt, polestar_dtype dtype, long rows, int n_out, int n_in) {
-    return mx_plan(x_fmt, dtype == POLESTAR_BF16, rows, n_out, n_in).ws_bytes;
+    return mx_few(x_fmt, rows, n_out, n_in) ? 0 : mx_plan(x_fmt, dtype == POLESTAR_BF16, rows, n_out, n_in).ws_bytes;
+}
+
+polestar_status mx_few_run(int x_fmt, bool bf16, const MxFewArgs& g, hipStream_t stream) {
+    const int nt = mx_few_nt(g.n_out);
+    if (x_fmt == POLESTAR_MXFP4) {
+        if (bf16) mx_launch_few<POLESTAR_MXFP4, true>(g, nt, stream);
+        else mx_launch_few<POLESTAR_MXFP4, false>(g, nt, stream);
+    } else {
+        if (bf16) mx_launch_few<POLESTAR_MXFP8, true>(g, nt, stream);
+        else mx_launch_few<POLESTAR_MXFP8, false>(g, nt, stream);
+    }
+    return launch_status();
 }
 
 polestar_status mx_gemm_run(int x_fmt, polestar_dtype dtype, MxGemmArgs g, void* workspace, hipStream_t stream) {
     const bool bf16 = dtype == POLESTAR_BF16;
+    if (mx_few(x_fmt, g.rows, g.n_out, g.n_in)) {
+        MxFewArgs f{};
+        static_cast<MxGemmArgs&>(f) = g;
+        return mx_few_run(x_fmt, bf16, f, stream);
+    }
     const MxPlan p = mx_plan(x_fmt, bf16, g.rows, g.n_out, g.n_in);
     g.part = static_cast<float*>(workspace);
     g.ksplit = p.ksplit;
@@ -470,6 +715,14 @@ polestar_status mx_gemm_run(int x_fmt, polestar_dtype dtype, MxGemmArgs g, void*
 // Rows and outputs that the kernels' indices hold.
 bool mx_shape_ok(long rows, int n_out, int n_in) {
     return n_in % 128 == 0 && n_out % 16 == 0 && rows <= (1L << 24) && n_out <= (1 << 22) && n_in <= (1 << 22);
+}
+
+// Rows that the product's kernel quantizes itself: up to 16, and few enough
+// workgroups that repeat it.  Against two launches, us: 4096 x 4096, bf16, 1 row 5.9
+// (5.9) and one launch less for the host, 16 rows 7.2 (7.0), fp32 4 rows 6.9 (6.8),
+// 16 rows 11.0 (7.4); 1024 x 256 3.7 (6.0); 12288 x 4096, bf16, 1 row 12.8 (10.3).
+bool mx_few_raw(bool bf16, long rows, int n_out, int n_in) {
+    return rows <= (bf16 ? 16 : 4) && static_cast<long>(ceil_div(n_out, 16 * mx_few_nt(n_out))) * n_in <= 1L << 20;
 }
 
 // Workspace of the quantized rows: codes, then scales.
@@ -519,7 +772,7 @@ extern "C" size_t polestar_mx_quantize_linear_workspace_size(int x_fmt, polestar
     using namespace ps;
     if (!mx_fmt_ok(x_fmt) || !dtype_ok(dtype) || batch <= 0 || n_rows <= 0 || n_out <= 0 || n_in <= 0) return 0;
     const long rows = static_cast<long>(batch) * n_rows;
-    if (!mx_shape_ok(rows, n_out, n_in)) return 0;
+    if (!mx_shape_ok(rows, n_out, n_in) || mx_few_raw(dtype == POLESTAR_BF16, rows, n_out, n_in)) return 0;
     return mx_rows_ws(x_fmt, rows, n_in) + mx_linear_ws(x_fmt, dtype, rows, n_out, n_in);
 }
 
@@ -536,7 +789,21 @@ extern "C" polestar_status polestar_mx_quantize_linear(int x_fmt, polestar_dtype
         !aligned16(y) || !aligned16(workspace) || batch > 65535)
         return POLESTAR_ERR_UNSUPPORTED;
     const size_t need = polestar_mx_quantize_linear_workspace_size(x_fmt, dtype, batch, n_rows, n_out, n_in);
-    if (workspace_bytes < need || !workspace) return POLESTAR_ERR_WORKSPACE;
+    if (workspace_bytes < need || (need > 0 && !workspace)) return POLESTAR_ERR_WORKSPACE;
+    if (mx_few_raw(dtype == POLESTAR_BF16, rows, n_out, n_in)) {
+        MxFewArgs f{};
+        f.w = w_codes;
+        f.ws = w_scales;
+        f.y = static_cast<char*>(y);
+        f.rows = rows;
+        f.n_out = n_out;
+        f.n_in = n_in;
+        f.raw = static_cast<const char*>(x);
+        f.seq = seq;
+        f.row_start = row_start;
+        f.n_rows = n_rows;
+        return mx_few_run(x_fmt, dtype == POLESTAR_BF16, f, stream);
+    }
     uint8_t* codes = static_cast<uint8_t*>(workspace);
     uint8_t* scales = codes + mx_rows_codes(x_fmt, rows, n_in);
     const polestar_status st =

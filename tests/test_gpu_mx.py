@@ -185,7 +185,7 @@ def _linear_bound(x, w, want, fmt, dtype):
 
 LINEAR = [(1, 128, 16), (1, 4096, 4096), (2, 256, 48), (5, 384, 272), (16, 1152, 64), (17, 640, 80), (32, 4096, 512),
           (33, 512, 144), (48, 896, 1040), (64, 384, 256), (65, 256, 272), (97, 3584, 1168), (130, 1024, 400),
-          (256, 512, 528), (300, 2176, 256), (513, 384, 784)]
+          (256, 512, 528), (300, 2176, 256), (513, 384, 784), (64, 128, 8336), (3, 896, 8208), (40, 640, 8224)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
