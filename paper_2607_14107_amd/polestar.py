@@ -600,6 +600,9 @@ def codec_gather(fmt: int, codes: torch.Tensor, scales: torch.Tensor, idx: torch
 # a layer's forward in the microscaling formats (include/polestar_mx.h)
 # ---------------------------------------------------------------------------
 
+# These calls are short (a few microseconds on the GPU for a block's rows), so
+# their checks are kept to one look at each tensor.
+
 def _mx_device(*tensors) -> int:
     """The index of the one device of the given tensors, which has to be the current one."""
     dev = tensors[0].get_device()
@@ -608,7 +611,7 @@ def _mx_device(*tensors) -> int:
             raise ValueError("tensors are on different devices")
     if dev < 0:
         raise ValueError("tensor must be on the GPU")
-    if dev != torch.cuda.current_device():
+    if dev != torch._C._cuda_getDevice():
         raise ValueError(f"tensors are on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
     return dev
 
@@ -652,21 +655,22 @@ def _mx_call(name: str, args: tuple, size, ws: torch.Tensor | None, dev: int, st
 
 
 def _mx_codes(fmt: int, codes: torch.Tensor, scales: torch.Tensor, what: str) -> int:
-    """Channels of a row held in codes [..., row bytes] and scales [..., n / 32]."""
-    n = 32 * scales.shape[-1]
-    if codes.shape[-1] != (n // 2 if fmt == MXFP4 else n) or codes.shape[:-1] != scales.shape[:-1]:
+    """Channels of a row held in codes [..., row bytes] and scales [..., n / 32] (as many rows of each)."""
+    per = 16 if fmt == MXFP4 else 32
+    ns = scales.size(-1)
+    if codes.size(-1) != per * ns or codes.numel() != per * scales.numel():
         raise ValueError(f"{what}: codes and scales do not match")
-    return n
+    return 32 * ns
 
 
 def _mx_row_stride(t: torch.Tensor, what: str) -> int:
     """Elements from row to row of t [batch][rows][heads][head_dim], whose heads lie one after another."""
     b, n, heads, hd = t.shape
-    s = t.stride()
     if t.numel() == 0:
         return heads * hd
-    rs = s[1] if n > 1 else (s[0] if b > 1 else heads * hd)
-    if (s[3] != 1 and hd > 1) or (s[2] != hd and heads > 1) or (b > 1 and s[0] != n * rs):
+    s0, s1, s2, s3 = t.stride()
+    rs = s1 if n > 1 else (s0 if b > 1 else heads * hd)
+    if (s3 != 1 and hd > 1) or (s2 != hd and heads > 1) or (b > 1 and s0 != n * rs):
         raise ValueError(f"{what}: rows must be equally spaced and whole")
     return rs
 
@@ -701,11 +705,12 @@ def mx_quantize(fmt: int, x: torch.Tensor, row_start: int = 0, n_rows: int | Non
 def mx_dequantize(fmt: int, codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, stream=None) -> torch.Tensor:
     """The values of codes [..., row bytes] and scales [..., n / 32] into out [..., n] (float32 or bfloat16)."""
     n = _mx_codes(fmt, codes, scales, "mx_dequantize")
-    if out.shape[-1] != n or out.shape[:-1] != codes.shape[:-1]:
+    values = out.numel()
+    if out.size(-1) != n or values != 32 * scales.numel():
         raise ValueError("mx_dequantize: shapes do not match")
     dev = _mx_device(codes, scales, out)
     _check("polestar_mx_dequantize", lib().polestar_mx_dequantize(
-        fmt, _dtype_code(out), out.numel() // n if n else 0, n, _mx_ptr(codes, torch.uint8),
+        fmt, _dtype_code(out), values // n if n else 0, n, _mx_ptr(codes, torch.uint8),
         _mx_ptr(scales, torch.uint8), _mx_ptr(out, out.dtype), _mx_stream(dev, stream)))
     return out
 
@@ -719,12 +724,13 @@ def mx_linear(x_fmt: int, x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes
               stream=None) -> torch.Tensor:
     """y[..., o] = sum_i x[..., i] w[o, i]: rows in MXFP8 or MXFP4, weights in MXFP4, y float32 or bfloat16."""
     n_in = _mx_codes(x_fmt, x_codes, x_scales, "mx_linear")
-    n_out = w_codes.shape[0]
+    n_out = w_codes.size(0)
+    rows = 32 * x_scales.numel() // n_in if n_in else 0
     if (_mx_codes(MXFP4, w_codes, w_scales, "mx_linear") != n_in or w_codes.dim() != 2
-            or y.shape[-1] != n_out or y.shape[:-1] != x_codes.shape[:-1]):
+            or y.size(-1) != n_out or y.numel() != rows * n_out):
         raise ValueError("mx_linear: shapes do not match")
     dev = _mx_device(x_codes, x_scales, w_codes, w_scales, y, workspace)
-    rows, dt = y.numel() // n_out, _dtype_code(y)
+    dt = _dtype_code(y)
     _mx_call("polestar_mx_linear", (
         x_fmt, dt, rows, n_in, n_out, _mx_ptr(x_codes, torch.uint8), _mx_ptr(x_scales, torch.uint8),
         _mx_ptr(w_codes, torch.uint8), _mx_ptr(w_scales, torch.uint8), _mx_ptr(y, y.dtype)),
@@ -742,7 +748,7 @@ def mx_quantize_linear(x_fmt: int, x: torch.Tensor, row_start: int, n_rows: int,
     """mx_quantize of rows [row_start, row_start + n_rows) of x [batch][seq][n_in], then mx_linear of them into
     y [batch][n_rows][n_out] (x's dtype)."""
     b, seq, n_in = x.shape
-    n_out = w_codes.shape[0]
+    n_out = w_codes.size(0)
     if (_mx_codes(MXFP4, w_codes, w_scales, "mx_quantize_linear") != n_in or w_codes.dim() != 2
             or y.shape != (b, n_rows, n_out)):
         raise ValueError("mx_quantize_linear: shapes do not match")
@@ -760,14 +766,15 @@ def residual_rmsnorm_mx(fmt: int, x: torch.Tensor, y: torch.Tensor | None, x_out
                         eps: float = 1e-5, stream=None) -> None:
     """x_out = x + y (float32; x_out may be x, y may be None), then codes and scales of RMSNorm(x_out) * gain.
     x [..., d], codes [..., row bytes], scales [..., d / 32]."""
-    d = x.shape[-1]
-    if (_mx_codes(fmt, codes, scales, "residual_rmsnorm_mx") != d or codes.shape[:-1] != x.shape[:-1]
+    d = x.size(-1)
+    values = x.numel()
+    if (_mx_codes(fmt, codes, scales, "residual_rmsnorm_mx") != d or values != 32 * scales.numel()
             or (y is not None and (y.shape != x.shape or x_out is None))
             or (x_out is not None and x_out.shape != x.shape) or (gain is not None and gain.shape != (d,))):
         raise ValueError("residual_rmsnorm_mx: shapes do not match")
     dev = _mx_device(x, y, x_out, codes, scales, gain)
     _check("polestar_residual_rmsnorm_mx", lib().polestar_residual_rmsnorm_mx(
-        fmt, BF16 if y is None else _dtype_code(y), x.numel() // d, d, _mx_ptr(x, torch.float32),
+        fmt, BF16 if y is None else _dtype_code(y), values // d, d, _mx_ptr(x, torch.float32),
         None if y is None else _mx_ptr(y, y.dtype), _mx_ptr(gain, torch.float32), float(eps),
         _mx_ptr(x_out, torch.float32), _mx_ptr(codes, torch.uint8), _mx_ptr(scales, torch.uint8),
         _mx_stream(dev, stream)))
