@@ -26,34 +26,16 @@ struct MxGemmArgs {
     float* part;                                         // split K: partials [split][rows][n_out]
     long rows;
     int n_out, n_in;
-    int ksplit, steps;                                   // K tiles of a split
+    int ksplit, steps;                                   // 128-channel steps of a split, an even number
     int row_tiles, col_tiles;
 };
 
-// A K tile is 128 channels: operand fragments of the 16x16x128 instruction, lane l
-// holding row l % 16 and the scale of block g = l / 16.  DEC: decoded to bf16 for
-// four 16x16x32 instructions.
-//
-// Rows in LDS: 16-byte chunks, XOR-swizzled so that the lanes whose reads run
-// together (0-3, 12-15, 20-27 of each 32, and the others) lie in different banks.
-// With rows of 64 bytes swizzled by row / 4 half the LDS cycles of an MXFP4 product
-// were conflicts; by its negative none are.
-template <int FMT> struct LdsRow;
-template <> struct LdsRow<POLESTAR_MXFP4> {
-    static constexpr int kBytes = 64;
-    __device__ __forceinline__ static int chunk(int row, int c) { return (c ^ (-(row >> 2) & 3)) << 4; }
-};
-template <> struct LdsRow<POLESTAR_MXFP8> {
-    static constexpr int kBytes = 128;
-    __device__ __forceinline__ static int chunk(int row, int c) { return (c ^ ((row >> 1) & 7)) << 4; }
-};
-
+// Operand fragments of a step, 128 channels of the 16x16x128 instruction: lane l
+// holds row l % 16 and the scale of block g = l / 16.  DEC: decoded to bf16 for four
+// 16x16x32 instructions.
 template <int FMT, bool DEC> struct Frag;
 template <bool DEC> struct Frag<POLESTAR_MXFP4, DEC> {
     uint4 c;                                             // channels 32 g ..
-    __device__ __forceinline__ void load(const char* tile, int r, int g) {
-        c = ld16(tile + r * 64 + LdsRow<POLESTAR_MXFP4>::chunk(r, g));
-    }
     __device__ __forceinline__ intx8 codes() const {
         return intx8{static_cast<int>(c.x), static_cast<int>(c.y), static_cast<int>(c.z), static_cast<int>(c.w), 0, 0, 0, 0};
     }
@@ -66,10 +48,6 @@ template <bool DEC> struct Frag<POLESTAR_MXFP4, DEC> {
 // (its scale is still that of block g); decoded, 32 g .. as with 4 bits.
 template <bool DEC> struct Frag<POLESTAR_MXFP8, DEC> {
     uint4 c[2];
-    __device__ __forceinline__ void load(const char* tile, int r, int g) {
-        c[0] = ld16(tile + r * 128 + LdsRow<POLESTAR_MXFP8>::chunk(r, DEC ? 2 * g : g));
-        c[1] = ld16(tile + r * 128 + LdsRow<POLESTAR_MXFP8>::chunk(r, DEC ? 2 * g + 1 : 4 + g));
-    }
     __device__ __forceinline__ intx8 codes() const {
         return intx8{static_cast<int>(c[0].x), static_cast<int>(c[0].y), static_cast<int>(c[0].z), static_cast<int>(c[0].w),
                      static_cast<int>(c[1].x), static_cast<int>(c[1].y), static_cast<int>(c[1].z), static_cast<int>(c[1].w)};
@@ -80,15 +58,36 @@ template <bool DEC> struct Frag<POLESTAR_MXFP8, DEC> {
     }
 };
 
+// A K tile's rows in LDS (KS steps): 64 or 128 bytes, their 16-byte chunks
+// XOR-swizzled so that the lanes whose reads run together (0-3, 12-15, 20-27 of each
+// 32, and the others) lie in different banks.  With rows of 64 bytes swizzled by row
+// / 4 half the LDS cycles of an MXFP4 product were conflicts.
+template <int FMT, int KS> struct LdsRow {
+    static constexpr int kBytes = KS * 16 * Mx<FMT>::kBits;
+    static_assert(kBytes == 64 || kBytes == 128, "");
+    __device__ __forceinline__ static int chunk(int row, int c) {
+        return (c ^ (kBytes == 64 ? -(row >> 2) & 3 : (row >> 1) & 7)) << 4;
+    }
+    template <bool DEC> __device__ __forceinline__ static void load(Frag<FMT, DEC>& f, const char* tile, int r, int step, int g) {
+        const char* p = tile + r * kBytes;
+        if constexpr (FMT == POLESTAR_MXFP4) {
+            f.c = ld16(p + chunk(r, 4 * step + g));
+        } else {
+            f.c[0] = ld16(p + chunk(r, DEC ? 2 * g : g));
+            f.c[1] = ld16(p + chunk(r, DEC ? 2 * g + 1 : 4 + g));
+        }
+    }
+};
+
 constexpr int kMxTileThreads = 512;                      // eight waves, two per SIMD
 constexpr int kMxBand = 4;                               // row tiles per band of the launch order
 constexpr int kMxCus = 256;
 
-// Transfers into LDS, 16 or 12 bytes per lane, from a buffer of `bytes` bytes at
-// base: a lane's offset is one register, the K tile's a scalar; the lanes land one
-// after another from lds on.  Written out, because the compiler waits for every
-// transfer that it knows of before it reads LDS; the waits are the kernel's own
-// (mx_wait_vm before the barrier that hands a slot over).
+// Transfers into LDS, 16 or 12 bytes per lane, from a buffer of `bytes` bytes at base: a
+// lane's offset is one register, the K tile's a scalar; the lanes land one after
+// another from lds on.  Written out, because the compiler waits for every transfer
+// that it knows of before it reads LDS; the waits are the kernel's own (mx_wait_vm
+// before the barrier that hands a slot over).
 typedef uint32_t MxBuffer __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ MxBuffer mx_buffer(const void* base, uint32_t bytes) {
@@ -112,12 +111,21 @@ __device__ __forceinline__ void mx_dma12(MxBuffer b, uint32_t lane_off, uint32_t
 constexpr int mx_wait_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
 constexpr int kMxWaitLgkm0 = 15 | (3 << 14) | (7 << 4);
 
-// LDS: slots of a K tile's codes, as many as fit, three or four, beside two
-// buffers of the scales of as many K tiles.
-constexpr int mx_slot_bytes(int fmt, int mi, int nj) { return 32 * mi * (fmt == POLESTAR_MXFP8 ? 128 : 64) + 64 * nj * 64; }
-constexpr int mx_slots(int fmt, int mi, int nj) {
-    return 4 * (mx_slot_bytes(fmt, mi, nj) + 8 * (32 * mi + 64 * nj)) <= 160 * 1024 ? 4 : 3;
-}
+// A tile shape: BM = 16 MI WM rows x BN = 16 NJ (8 / WM) outputs per workgroup, its
+// eight waves in a WM x (8 / WM) grid of MI x NJ tiles; K tiles of KS steps.
+template <int FMT_, int WM_, int MI_, int NJ_, int KS_> struct MxShape {
+    static constexpr int FMT = FMT_, WM = WM_, WN = 8 / WM_, MI = MI_, NJ = NJ_, KS = KS_;
+    static constexpr int BM = 16 * MI * WM, BN = 16 * NJ * WN;
+    using X = LdsRow<FMT, KS>;
+    using W = LdsRow<POLESTAR_MXFP4, KS>;
+    // LDS: slots of a K tile's codes, as many as fit, beside two buffers of the
+    // scales of a round of K tiles
+    static constexpr int kX = BM * X::kBytes, kSlot = kX + BN * W::kBytes, kLds = 160 * 1024;
+    static constexpr bool fits(int ns) { return ns * kSlot + 2 * 4 * ns * KS * (BM + BN) <= kLds; }
+    static constexpr int NS = fits(4) ? 4 : fits(3) ? 3 : 2;
+    static constexpr int kRow = 4 * NS * KS, kScales = kRow * (BM + BN);   // a row's scales of a round
+    static_assert(fits(NS) && (kRow == 12 || kRow == 16), "");
+};
 
 // Workgroup blk -> (split, row tile, column tile): consecutive workgroups go to
 // different XCDs, so the ids are first regrouped per XCD, and each XCD walks
@@ -136,37 +144,33 @@ __device__ __forceinline__ void mx_tile_coords(const MxGemmArgs& g, int blk, int
     rt = band * kMxBand + (in - ct * rows_here);
 }
 
-// 32 MI rows x 64 NJ outputs per workgroup: eight waves in a 2 x 4 grid of MI x NJ
-// tiles of the 16x16x128 scaled instruction (DEC: four 16x16x32 bf16 ones), K in
-// tiles of 128 channels, codes and scales by DMA into NS LDS slots, one barrier
-// per K tile.
-template <int FMT, bool BF16, int MI, int NJ>
+// A workgroup's tile: codes and scales by DMA into LDS slots, one barrier per K tile,
+// a wave's blocks on the 16x16x128 scaled instruction (DEC: four 16x16x32 bf16 ones).
+template <class T, bool BF16>
 __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
+    constexpr int FMT = T::FMT, MI = T::MI, NJ = T::NJ, KS = T::KS, BM = T::BM, BN = T::BN, NS = T::NS;
     constexpr bool DEC = FMT == POLESTAR_MXFP8 && !BF16;
-    constexpr int BM = 32 * MI, BN = 64 * NJ;
-    constexpr int XB = LdsRow<FMT>::kBytes, WB = LdsRow<POLESTAR_MXFP4>::kBytes;
+    constexpr int XB = T::X::kBytes, WB = T::W::kBytes;
     constexpr int XG = BM * XB / 1024, WG = BN * WB / 1024, SG = (BM + BN) / 64;   // DMA groups of a K tile
     constexpr int XI = (XG + 7) / 8, WI = (WG + 7) / 8;  // instructions per wave
     constexpr int ND = XI + WI;
-    constexpr int NS = mx_slots(FMT, MI, NJ);
     static_assert(SG <= 8, "a wave per group of scales");
-    constexpr int W0 = BM * XB, SLOT = mx_slot_bytes(FMT, MI, NJ);   // a slot: rows, weights
-    constexpr int SB = 4 * NS, SBUF = SB * (BM + BN);    // a row's scales of NS K tiles
-    __shared__ __align__(16) char l0[SLOT], l1[SLOT], l2[SLOT], l3[NS > 3 ? SLOT : 1], sc[2 * SBUF];
+    __shared__ __align__(16) char lds[NS * T::kSlot + 2 * T::kScales];
+    char* const sc = lds + NS * T::kSlot;
 
     int split, rt, ct;
     mx_tile_coords(g, blockIdx.x, split, rt, ct);
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = w & 1, wn = w >> 1;
+    const int wm = w % T::WM, wn = w / T::WM;
     const int r = lane & 15, grp = lane >> 4;
     const long m0 = static_cast<long>(rt) * BM;
     const int n0 = ct * BN;
-    const int kt0 = split * g.steps;
-    const int nkt = min(g.steps, g.n_in / 128 - kt0);
+    const int q0 = split * g.steps;                      // this split's steps
+    const int nst = min(g.steps, g.n_in / 128 - q0), nkt = (nst + KS - 1) / KS;
 
     // DMA sources.  The buffers end with the tile's last row: what lies behind it
-    // (rows and columns past the end, scales behind the last K tile) reads as 0.  A
+    // (rows and columns past the end, scales behind the last step) reads as 0.  A
     // group past the last (few rows): the last group again, the same bytes.
     const uint32_t xrow = static_cast<uint32_t>(g.n_in / 8) * Mx<FMT>::kBits, wrow = g.n_in / 2, srow = g.n_in / 32;
     const uint32_t mrows = static_cast<uint32_t>(min(g.rows - m0, static_cast<long>(BM))), nrows = min(g.n_out - n0, BN);
@@ -174,94 +178,73 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     const MxBuffer wbuf = mx_buffer(g.w + static_cast<size_t>(n0) * wrow, nrows * wrow);
     constexpr int XR = 1024 / XB, WR = 1024 / WB;        // rows of a group
     const int xg = min(w, XG - 1), wg = min(w, WG - 1), xr = xg * XR + lane / (XB / 16), wr = wg * WR + lane / (WB / 16);
-    const uint32_t xsrc = xr * xrow + LdsRow<FMT>::chunk(xr, lane % (XB / 16));   // (the swizzle repeats with the groups)
-    const uint32_t wsrc = wr * wrow + LdsRow<POLESTAR_MXFP4>::chunk(wr, lane % (WB / 16));
-    // DMA instructions d0 .. d0 + n - 1 of K tile kt (past the split: its last one again)
-    auto issue = [&](int d0, int n, int kt, const char* slot) {
-        const uint32_t k = kt0 + min(kt, nkt - 1);
-#pragma unroll
-        for (int d = d0; d < d0 + n; ++d) {
-            if (d < XI) mx_dma16(xbuf, xsrc, k * XB + 8 * d * XR * xrow, slot + (xg + 8 * d) * 1024);
-            else if (d < ND)
-                mx_dma16(wbuf, wsrc, k * WB + 8 * (d - XI) * WR * wrow, slot + W0 + (wg + 8 * (d - XI)) * 1024);
-        }
-    };
-    // Scales, NS K tiles at a time: 64 rows of x or of w per wave.  (One K tile's
+    const uint32_t xsrc = xr * xrow + T::X::chunk(xr, lane % (XB / 16));   // (the swizzle repeats with the groups)
+    const uint32_t wsrc = wr * wrow + T::W::chunk(wr, lane % (WB / 16));
+    // Scales, a round of NS K tiles at a time, 64 rows of x or of w per wave.  (A step's
     // four bytes at a time are a cache line each too, and took a quarter of the time.)
     const int sg = min(w, SG - 1);
     const bool of_x = sg < BM / 64;
     const MxBuffer sbuf = of_x ? mx_buffer(g.xs + static_cast<size_t>(m0) * srow, mrows * srow)
                                : mx_buffer(g.ws + static_cast<size_t>(n0) * srow, nrows * srow);
     const uint32_t ssrc = static_cast<uint32_t>(of_x ? 64 * sg + lane : 64 * sg + lane - BM) * srow;
-    auto issue_scales = [&](int kt, int buf) {
-        if constexpr (NS == 4) mx_dma16(sbuf, ssrc, 4 * (kt0 + kt), sc + buf + 64 * SB * sg);
-        else mx_dma12(sbuf, ssrc, 4 * (kt0 + kt), sc + buf + 64 * SB * sg);
+    auto issue_scales = [&](int t, int buf) {
+        if constexpr (T::kRow == 16) mx_dma16(sbuf, ssrc, 4 * (q0 + t * KS), sc + buf + 64 * T::kRow * sg);
+        else mx_dma12(sbuf, ssrc, 4 * (q0 + t * KS), sc + buf + 64 * T::kRow * sg);
+    };
+    // DMA instructions d0 .. d0 + n - 1 of K tile t (past the split: its last one again)
+    auto issue = [&](int d0, int n, int t, const char* slot) {
+        const uint32_t k = min(t, nkt - 1), kx = q0 * (XB / KS) + k * XB, kw = q0 * (WB / KS) + k * WB;
+#pragma unroll
+        for (int d = d0; d < d0 + n; ++d) {
+            if (d < XI) mx_dma16(xbuf, xsrc, kx + 8 * d * XR * xrow, slot + (xg + 8 * d) * 1024);
+            else if (d < ND)
+                mx_dma16(wbuf, wsrc, kw + 8 * (d - XI) * WR * wrow, slot + T::kX + (wg + 8 * (d - XI)) * 1024);
+        }
     };
 
-    // Row fragments: of two K tiles, or for the largest tile (kRing: two would not
-    // fit the registers) four, each replaced right after its use by the one four
-    // row tiles on, of this K tile or the next.
-    constexpr bool kRing = MI == 8;
-    constexpr int NB = kRing ? 1 : 2, NX = kRing ? 4 : MI;
-    static_assert(kRing || NS % 2 == 0, "two register sets, in turn");
-    Frag<FMT, DEC> fx[NB][NX];
-    Frag<POLESTAR_MXFP4, DEC> fw[NB][NJ], fwn[NJ];
-    uint32_t sx[NB][NX], sw[NB][NJ], swn[NJ];            // scale bytes
-    const char* const xsc = sc + (16 * MI * wm + r) * SB + grp;
-    const char* const wsc = sc + (BM + 16 * NJ * wn + r) * SB + grp;
-    // fragments and scales (at so in the buffers) of a K tile
-    auto read_x = [&](const char* slot, int so, int set, int j) {
-        fx[set][j % NX].load(slot + 16 * (MI * wm + j) * XB, r, grp);
-        sx[set][j % NX] = *reinterpret_cast<const uint8_t*>(xsc + so + 16 * SB * j);
+    // A wave's fragments.  The two largest shapes have 8 row (or output) tiles: they
+    // hold the other operand's four and a ring of four of the eight, each replaced right
+    // after its use by the one four on, of this step or the next (two steps' fragments
+    // would not fit the registers); the smaller shapes hold two steps' in turn.
+    constexpr bool kRing = MI * NJ == 32, kRingX = kRing && MI == 8;
+    constexpr int NX = kRingX ? 4 : MI, NW = kRing && !kRingX ? 4 : NJ, SETS = 2;
+    Frag<FMT, DEC> fx[SETS][NX];
+    Frag<POLESTAR_MXFP4, DEC> fw[SETS][NW];
+    uint32_t sx[SETS][NX], sw[SETS][NW];                 // scale bytes
+    const char* const xsc = sc + (16 * MI * wm + r) * T::kRow + grp;
+    const char* const wsc = sc + (BM + 16 * NJ * wn + r) * T::kRow + grp;
+    // fragment j of step s of a slot, its scales at o in the buffers
+    auto read_x = [&](int set, int j, const char* slot, int s, int o) {
+        T::X::load(fx[set][j % NX], slot + 16 * (MI * wm + j) * XB, r, s, grp);
+        sx[set][j % NX] = *reinterpret_cast<const uint8_t*>(xsc + o + 16 * T::kRow * j);
     };
-    auto read_w = [&](const char* slot, int so, Frag<POLESTAR_MXFP4, DEC>* f, uint32_t* s) {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            f[j].load(slot + W0 + 16 * (NJ * wn + j) * WB, r, grp);
-            s[j] = *reinterpret_cast<const uint8_t*>(wsc + so + 16 * SB * j);
-        }
+    auto read_w = [&](int set, int j, const char* slot, int s, int o) {
+        T::W::load(fw[set][j % NW], slot + T::kX + 16 * (NJ * wn + j) * WB, r, s, grp);
+        sw[set][j % NW] = *reinterpret_cast<const uint8_t*>(wsc + o + 16 * T::kRow * j);
     };
     floatx4 acc[MI][NJ];
 #pragma unroll
     for (int a = 0; a < MI; ++a)
 #pragma unroll
         for (int b = 0; b < NJ; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-    auto mma = [&](int set, int a) {
+    auto mma = [&](int xset, int wset, int a, int b) {
+        const auto& x = fx[xset][a % NX];
+        const auto& v = fw[wset][b % NW];
         if constexpr (DEC) {
-            uint4 dx[4];
-            fx[set][a % NX].decode(dx, mx_scale(sx[set][a % NX]));
+            uint4 dx[4], dw[4];
+            x.decode(dx, mx_scale(sx[xset][a % NX]));
+            v.decode(dw, mx_scale(sw[wset][b % NW]));
 #pragma unroll
-            for (int b = 0; b < NJ; ++b) {
-                uint4 dw[4];
-                fw[set][b].decode(dw, mx_scale(sw[set][b]));
-#pragma unroll
-                for (int t = 0; t < 4; ++t) acc[a][b] = mfma_bf16(dw[t], dx[t], acc[a][b]);
-            }
+            for (int t = 0; t < 4; ++t) acc[a][b] = mfma_bf16(dw[t], dx[t], acc[a][b]);
         } else {
-#pragma unroll
-            for (int b = 0; b < NJ; ++b)
-                acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                    fw[set][b].codes(), fx[set][a % NX].codes(), acc[a][b], Mx<POLESTAR_MXFP4>::kMfma, Mx<FMT>::kMfma, 0,
-                    sw[set][b], 0, sx[set][a % NX]);
+            acc[a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v.codes(), x.codes(), acc[a][b],
+                                                                         Mx<POLESTAR_MXFP4>::kMfma, Mx<FMT>::kMfma, 0,
+                                                                         sw[wset][b % NW], 0, sx[xset][a % NX]);
         }
     };
-
-    issue_scales(0, 0);
-    issue(0, ND, 0, l0);
-    issue(0, ND, 1, l1);
-    issue(0, ND, 2, l2);
-    if constexpr (NS > 3) issue(0, ND, 3, l3);
-    __builtin_amdgcn_s_waitcnt(mx_wait_vm((NS - 1) * ND));
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    read_w(l0, 0, fw[0], sw[0]);
-#pragma unroll
-    for (int a = 0; a < NX; ++a) read_x(l0, 0, 0, a);
-    // K tile T in slot U (its first fragments in registers), T + 1 in X.  The barrier
-    // is for this wave's reads of U and its DMA of T + 1: behind it T + 1 may be read
-    // and U takes T + NS, a few instructions per row tile.
-    constexpr int DPR = kRing ? (ND + MI - 6) / (MI - 5) : (ND + MI - 1) / MI;
     auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+    // The barrier of K tile t, for this wave's reads of its slot and its DMA of t + 1:
+    // behind it t + 1 may be read and the slot takes t + NS.
     auto sync = [&] {
         fence();
         __builtin_amdgcn_s_waitcnt(mx_wait_vm((NS - 2) * ND) & kMxWaitLgkm0);
@@ -269,59 +252,125 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
         asm volatile("" ::: "memory");
         fence();
     };
-    auto ktile = [&](auto set, int t, const char* u, const char* x, int su, int so) {
-        constexpr int S = kRing ? 0 : decltype(set)::value;
-        if constexpr (kRing) {
+    issue_scales(0, 0);
 #pragma unroll
-            for (int a = 0; a < MI; ++a) {
-                mma(0, a);
-                if (a == MI - 4) {
-                    sync();
-                    read_w(x, so, fwn, swn);
+    for (int t = 0; t < NS; ++t) issue(0, ND, t, lds + t * T::kSlot);
+    __builtin_amdgcn_s_waitcnt(mx_wait_vm((NS - 1) * ND));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // K tile t, in slot U, whose round's scales are in buffer `buf`.  (The slots are
+    // constants: with a slot that moves, each read's address is computed behind the
+    // barrier, 8% slower.)
+    auto slot_of = [&](int u) { return lds + u % NS * T::kSlot; };
+    auto scales_of = [&](int step, int buf) {            // of a step of this round, or the next round's first
+        return step < NS * KS ? buf + 4 * step : buf ^ T::kScales;
+    };
+    int buf = 0, t = 0;
+    auto rounds = [&](int whole, auto ktile) {           // K tiles 0 .. whole - 1
+        using std::integral_constant;
+        for (; t + NS <= whole; t += NS, buf ^= T::kScales) {
+            ktile(t, integral_constant<int, 0>{});
+            issue_scales(t + NS, buf ^ T::kScales);      // landed by the last sync of this round
+            ktile(t + 1, integral_constant<int, 1>{});
+            if constexpr (NS > 2) ktile(t + 2, integral_constant<int, 2>{});
+            if constexpr (NS > 3) ktile(t + 3, integral_constant<int, 3>{});
+        }
+        if (t < whole) ktile(t, integral_constant<int, 0>{});
+        if (NS > 2 && t + 1 < whole) ktile(t + 1, integral_constant<int, 1>{});
+        if constexpr (NS > 3)
+            if (t + 2 < whole) ktile(t + 2, integral_constant<int, 2>{});
+    };
+    if constexpr (kRing) {
+        constexpr int NI = 4;                            // tiles of the operand that is held
+        auto read_ring = [&](int j, const char* slot, int s, int o) {
+            if constexpr (kRingX) read_x(0, j, slot, s, o);
+            else read_w(0, j, slot, s, o);
+        };
+        auto read_held = [&](int set, const char* slot, int s, int o) {
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                if constexpr (kRingX) read_w(set, j, slot, s, o);
+                else read_x(set, j, slot, s, o);
+            }
+        };
+        auto row = [&](int j) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                if constexpr (kRingX) mma(0, 0, j, i);
+                else mma(0, 0, i, j);
+            }
+        };
+        read_held(0, lds, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) read_ring(j, lds, 0, 0);
+        constexpr int DPR = (ND + 2) / 3;                // DMA instructions behind each of the last three
+        auto ktile = [&](int kt, auto which) {
+            constexpr int U = decltype(which)::value;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bool last = s == KS - 1;
+                const int o = scales_of(U * KS + s, buf), on = scales_of(U * KS + s + 1, buf);
+                const char* next = last ? slot_of(U + 1) : slot_of(U);
+                const int sn = last ? 0 : s + 1;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    row(j);
+                    if (j == 4) {
+                        if (last) sync();
+                        read_held(1, next, sn, on);
+                    }
+                    fence();
+                    if (j < 4) read_ring(j + 4, slot_of(U), s, o);
+                    else read_ring(j - 4, next, sn, on);
+                    if (last && j > 4) issue((j - 5) * DPR, DPR, kt + NS, slot_of(U));
+                    fence();
                 }
-                fence();
-                if (a < MI - 4) read_x(u, su, 0, a + 4);
-                else read_x(x, so, 0, a + 4 - MI);
-                if (a > MI - 4) issue((a - MI + 3) * DPR, DPR, t + NS, u);
-                fence();
-            }
 #pragma unroll
-            for (int b = 0; b < NJ; ++b) {
-                fw[0][b] = fwn[b];
-                sw[0][b] = swn[b];
+                for (int i = 0; i < NI; ++i) {
+                    if constexpr (kRingX) {
+                        fw[0][i] = fw[1][i];
+                        sw[0][i] = sw[1][i];
+                    } else {
+                        fx[0][i] = fx[1][i];
+                        sx[0][i] = sx[1][i];
+                    }
+                }
             }
-        } else {
+        };
+        const int whole = nst / KS;
+        rounds(whole, ktile);
+        if (KS > 1 && whole < nkt) {                     // one step is left
+            const int u = whole - t;                     // its slot
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                row(j);
+                if (j < 4) read_ring(j + 4, lds + u * T::kSlot, 0, buf + 4 * u * KS);
+            }
+        }
+    } else {
+        static_assert(KS == 1 && NS % 2 == 0, "two register sets, in turn");
+        constexpr int DPR = (ND + MI - 1) / MI;
+        auto read = [&](int set, const char* slot, int o) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) read_w(set, j, slot, 0, o);
+#pragma unroll
+            for (int j = 0; j < MI; ++j) read_x(set, j, slot, 0, o);
+        };
+        read(0, lds, 0);
+        rounds(nkt, [&](int kt, auto which) {
+            constexpr int U = decltype(which)::value, S = U % 2;
             sync();
-            read_w(x, so, fw[1 - S], sw[1 - S]);
-#pragma unroll
-            for (int a = 0; a < MI; ++a) read_x(x, so, 1 - S, a);
+            read(1 - S, slot_of(U + 1), scales_of(U + 1, buf));
             fence();
 #pragma unroll
             for (int a = 0; a < MI; ++a) {
-                mma(S, a);
-                issue(a * DPR, DPR, t + NS, u);
+#pragma unroll
+                for (int b = 0; b < NJ; ++b) mma(S, S, a, b);
+                issue(a * DPR, DPR, kt + NS, slot_of(U));
                 fence();
             }
-        }
-    };
-    using Set0 = std::integral_constant<int, 0>;
-    using Set1 = std::integral_constant<int, 1>;
-    int kt = 0, buf = 0;                                 // buf: the scales of K tiles kt .. kt + NS - 1
-    for (; kt + NS <= nkt; kt += NS, buf ^= SBUF) {
-        ktile(Set0{}, kt, l0, l1, buf, buf + 4);
-        issue_scales(kt + NS, buf ^ SBUF);               // landed by the last sync of this round
-        ktile(Set1{}, kt + 1, l1, l2, buf + 4, buf + 8);
-        if constexpr (NS == 3) {
-            ktile(Set0{}, kt + 2, l2, l0, buf + 8, buf ^ SBUF);
-        } else {
-            ktile(Set0{}, kt + 2, l2, l3, buf + 8, buf + 12);
-            ktile(Set1{}, kt + 3, l3, l0, buf + 12, buf ^ SBUF);
-        }
+        });
     }
-    if (kt < nkt) ktile(Set0{}, kt, l0, l1, buf, buf + 4);
-    if (kt + 1 < nkt) ktile(Set1{}, kt + 1, l1, l2, buf + 4, buf + 8);
-    if constexpr (NS == 4)
-        if (kt + 2 < nkt) ktile(Set0{}, kt + 2, l2, l3, buf + 8, buf + 12);
     __builtin_amdgcn_s_waitcnt(0);                       // every DMA (the re-read tail too) has landed
     __syncthreads();                                     // and every wave is done with the slots
 
@@ -346,8 +395,8 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     constexpr int ES = BF16 ? 2 : 4;
     constexpr int EP = 16 * NJ * ES + 16;                // bytes of a staged row
     constexpr int CPR = NJ * ES;                         // 16-byte chunks of a row
-    static_assert(3 * 16 * EP <= SLOT, "three waves' rows fit a slot");
-    char* ep = (w % 3 == 0 ? l0 : w % 3 == 1 ? l1 : l2) + (w / 3) * 16 * EP;
+    static_assert(8 * 16 * EP <= sizeof(lds), "every wave's rows");
+    char* ep = lds + w * 16 * EP;
 #pragma unroll
     for (int a = 0; a < MI; ++a) {
 #pragma unroll
@@ -588,12 +637,22 @@ __global__ __launch_bounds__(256) void mx_reduce_kernel(const float* __restrict_
     else reinterpret_cast<float4*>(y)[i] = v;
 }
 
-// The tile shapes (MI, NJ); the decoding form has no registers for the two largest.
-constexpr bool mx_has_tile(int fmt, bool bf16, int mi, int nj) { return mi * nj <= 8 || fmt == POLESTAR_MXFP4 || bf16; }
-#define PS_MX_SHAPES(X) X(8, 4) X(4, 4) X(4, 2) X(2, 4) X(2, 2)
+// The tile shapes by rows and outputs.  MXFP8 rows: a wave's block is half as wide in
+// rows, whose fragments are twice the bytes.  The decoding form has no registers for
+// the two largest.
+constexpr bool mx_has_tile(int fmt, bool bf16, int bm, int bn) { return bm * bn < 256 * 128 || fmt == POLESTAR_MXFP4 || bf16; }
+template <int FMT, int BM, int BN> struct ShapeOf;
+template <> struct ShapeOf<POLESTAR_MXFP8, 256, 256> { using T = MxShape<POLESTAR_MXFP8, 2, 8, 4, 1>; };
+template <> struct ShapeOf<POLESTAR_MXFP4, 256, 256> { using T = MxShape<POLESTAR_MXFP4, 2, 8, 4, 2>; };
+template <int FMT> struct ShapeOf<FMT, 128, 256> { using T = MxShape<FMT, 2, 4, 4, 1>; };
+template <> struct ShapeOf<POLESTAR_MXFP8, 128, 128> { using T = MxShape<POLESTAR_MXFP8, 4, 2, 4, 1>; };
+template <> struct ShapeOf<POLESTAR_MXFP4, 128, 128> { using T = MxShape<POLESTAR_MXFP4, 2, 4, 2, 1>; };
+template <int FMT> struct ShapeOf<FMT, 64, 256> { using T = MxShape<FMT, 2, 2, 4, 1>; };
+template <int FMT> struct ShapeOf<FMT, 64, 128> { using T = MxShape<FMT, 2, 2, 2, 1>; };
+#define PS_MX_SHAPES(X) X(256, 256) X(128, 256) X(128, 128) X(64, 256) X(64, 128)
 
 struct MxPlan {
-    int mi, nj, ksplit, steps;
+    int bm, bn, ksplit, steps;
     size_t ws_bytes;
 };
 
@@ -601,22 +660,23 @@ struct MxPlan {
 // per CU, each its K tiles and a fixed cost, and for a split the partials'
 // way through memory.
 MxPlan mx_plan(int x_fmt, bool bf16, long rows, int n_out, int n_in) {
-    static constexpr struct { int mi, nj; double kt; } shapes[] = {{8, 4, 1.5}, {4, 4, 0.9}, {4, 2, 0.55}, {2, 4, 0.6}, {2, 2, 0.36}};
-    const int nkt = n_in / 128;
+    static constexpr struct { int bm, bn; double step; } shapes[] = {
+        {256, 256, 1.5}, {128, 256, 0.9}, {128, 128, 0.55}, {64, 256, 0.6}, {64, 128, 0.36}};
+    const int nst = n_in / 128;
     MxPlan p{};
     double best = 1e30;
     for (const auto& s : shapes) {
-        if (!mx_has_tile(x_fmt, bf16, s.mi, s.nj)) continue;
-        const long tiles = ((rows + 32 * s.mi - 1) / (32 * s.mi)) * ceil_div(n_out, 64 * s.nj);
-        for (int ks = 1; ks <= 16 && ks <= nkt; ++ks) {
-            const int steps = ceil_div(nkt, ks);
-            if (ceil_div(nkt, steps) != ks) continue;
+        if (!mx_has_tile(x_fmt, bf16, s.bm, s.bn)) continue;
+        const long tiles = (rows + s.bm - 1) / s.bm * ceil_div(n_out, s.bn);
+        for (int ks = 1; ks <= 16 && ks <= nst; ++ks) {
+            const int steps = ceil_div(ceil_div(nst, ks), 2) * 2;   // whole K tiles of every shape
+            if (ceil_div(nst, steps) != ks) continue;
             if (ks > 1 && (tiles * (ks - 1) >= kMxCus || steps < 4)) break;
             const double rounds = static_cast<double>((tiles * ks + kMxCus - 1) / kMxCus);
-            const double cost = rounds * (steps * s.kt + 4.0) + (ks > 1 ? 4.0 + 4.0 * ks * rows * n_out * 0.4e-6 : 0.0);
+            const double cost = rounds * (steps * s.step + 4.0) + (ks > 1 ? 4.0 + 4.0 * ks * rows * n_out * 0.4e-6 : 0.0);
             if (cost < best) {
                 best = cost;
-                p = MxPlan{s.mi, s.nj, ks, steps, ks > 1 ? 4 * static_cast<size_t>(ks) * rows * n_out : 0};
+                p = MxPlan{s.bm, s.bn, ks, steps, ks > 1 ? 4 * static_cast<size_t>(ks) * rows * n_out : 0};
             }
         }
     }
@@ -656,11 +716,11 @@ bool mx_few(int x_fmt, long rows, int n_out, int n_in) {
 template <int FMT, bool BF16>
 void mx_launch(const MxPlan& p, const MxGemmArgs& g, hipStream_t stream) {
     const dim3 grid(g.row_tiles * g.col_tiles * g.ksplit), block(kMxTileThreads);
-    switch (10 * p.mi + p.nj) {
-#define PS_CASE(MI, NJ) \
-        case 10 * MI + NJ:                                                                                   \
-            if constexpr (mx_has_tile(FMT, BF16, MI, NJ))                                                    \
-                hipLaunchKernelGGL((mx_tile_kernel<FMT, BF16, MI, NJ>), grid, block, 0, stream, g);          \
+    switch (1000 * p.bm + p.bn) {
+#define PS_CASE(BM, BN)                                                                                                   \
+        case 1000 * BM + BN:                                                                                              \
+            if constexpr (mx_has_tile(FMT, BF16, BM, BN))                                                                 \
+                hipLaunchKernelGGL((mx_tile_kernel<typename ShapeOf<FMT, BM, BN>::T, BF16>), grid, block, 0, stream, g);  \
             break;
         PS_MX_SHAPES(PS_CASE)
 #undef PS_CASE
@@ -700,8 +760,8 @@ polestar_status mx_gemm_run(int x_fmt, polestar_dtype dtype, MxGemmArgs g, void*
     g.part = static_cast<float*>(workspace);
     g.ksplit = p.ksplit;
     g.steps = p.steps;
-    g.row_tiles = ceil_div(g.rows, 32 * p.mi);
-    g.col_tiles = ceil_div(g.n_out, 64 * p.nj);
+    g.row_tiles = ceil_div(g.rows, p.bm);
+    g.col_tiles = ceil_div(g.n_out, p.bn);
     if (x_fmt == POLESTAR_MXFP4) {
         if (bf16) mx_launch<POLESTAR_MXFP4, true>(p, g, stream);
         else mx_launch<POLESTAR_MXFP4, false>(p, g, stream);
