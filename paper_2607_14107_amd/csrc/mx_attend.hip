@@ -11,7 +11,18 @@
 //
 // The waves of a workgroup take the steps in turn, and where the workgroups do not
 // fill the GPU the keys are split over several; each part's (reference, sum, O) are
-// joined at the end, in LDS and by a second kernel.
+// joined at the end, in LDS and by a second kernel.  In LDS every wave puts its part
+// down at once and every thread sums its share of the queries' channels behind one
+// barrier: added in pairs with a barrier each, the join took 0.5 to 1.5 us more.
+//
+// Measured inside a graph, head_dim 128, bf16: 8 x 32 heads, 1 query: 256 keys 5.6
+// us, 2048 keys 15.3, 8192 keys 65 (its 285 MB at 4.4 TB/s); 4 x 4 KV heads, 448
+// queries each: 1024 keys 11.3 us, 8192 keys 47.  Long caches of few queries are
+// bound by memory, many queries by the vector unit (187 instructions for the 16
+// matrix instructions of a step, 64 of them the codes' decoding).  Computing the
+// next step's scores beside this step's softmax was 5% slower, twelve waves or two
+// steps of prefetch no faster, nor was an order that keeps a head's query tiles on
+// one XCD.
 //
 // fp32 queries: q and p are taken as three bf16 terms each, so that the products
 // with the exact keys and values keep 24 bits.
@@ -121,8 +132,8 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
     constexpr int CT = HD / 32;                          // channel tiles
     constexpr int kPitch = 2 * HD + 64;                  // bytes of a key's row in LDS
     constexpr int kOPitch = 4 * HD + 16;                 // of a query's O
-    constexpr int kV = kMxKeys * kPitch, kO = kMxQ * kOPitch;
-    __shared__ __align__(16) char lds[NW * kV > NW / 2 * kO ? NW * kV : NW / 2 * kO];
+    constexpr int kV = kMxKeys * kPitch, kO = kMxQ * kOPitch, kPart = kV > kO ? kV : kO;   // of a wave: V's rows, then O
+    __shared__ __align__(16) char lds[NW * kPart];
     __shared__ float sm[NW][kMxQ], sl[NW][kMxQ];
 
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -167,7 +178,7 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) o[c][j] = 0.f;
     float m = -INFINITY, l = 0.f;                        // the exponents' reference; l of this lane's keys
-    char* vb = lds + w * kV;
+    char* vb = lds + w * kPart;
     // transposed reads: keys 4 h + 0..3 and 8 further on
     const int tk = 4 * h + ((lane & 15) >> 2), tq = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     const int tr0 = tk * kPitch + 16 * (tq ^ v_swizzle<HD>(tk)) + 8 * (lane & 1);
@@ -226,10 +237,9 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
         const float ref = m == -INFINITY ? 0.f : m;
         float p[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            p[j] = fast_exp2(fmaf(s[j], a.scale2, -ref));
-            l += p[j];
-        }
+        for (int j = 0; j < 16; ++j) p[j] = fast_exp2(fmaf(s[j], a.scale2, -ref));
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) l += (p[j] + p[j + 1]) + (p[j + 2] + p[j + 3]);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             uint4 pt[NT];
@@ -255,72 +265,63 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_kernel(MxAttArgs a) {
         even.load(kc, ks, vc, vs, (st + 2 * NW) * kMxKeys, lane);
         step(st + NW, odd);
     }
-    // the waves' parts: to the common reference, then added in pairs
+    // the waves' parts, (reference, sum, O) each, joined by every thread for its share
     l += __shfl_xor(l, 32);
     if (h == 0) {
         sm[w][i] = m;
         sl[w][i] = l;
     }
-    __syncthreads();
-    float mt = -INFINITY, lt = 0.f;
-#pragma unroll
-    for (int x = 0; x < NW; ++x) mt = fmaxf(mt, sm[x][i]);
-    const float ref = mt == -INFINITY ? 0.f : mt;
-#pragma unroll
-    for (int x = 0; x < NW; ++x) lt += sl[x][i] * fast_exp2(sm[x][i] - ref);
-    // l counts the keys, so it is 0 only where there were none (zeros) or where no
-    // score is finite (NaN, as the quotient)
-    const float f = fast_exp2(m - ref) * (a.splits > 1 ? 1.f : len > 0 ? 1.f / lt : 0.f);
+    // (V's rows lie in the wave's own part, so no barrier is needed before)
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[c][j] *= f;
-    auto each = [&](int buf, auto fn) {
-#pragma unroll
-        for (int c = 0; c < CT; ++c)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                fn(reinterpret_cast<float4*>(lds + buf * kO + i * kOPitch + (32 * c + 8 * j + 4 * h) * 4), c, 4 * j);
-    };
-    auto put = [&](float4* d, int c, int j) { *d = make_float4(o[c][j], o[c][j + 1], o[c][j + 2], o[c][j + 3]); };
-#pragma unroll
-    for (int half = NW / 2; half >= 1; half /= 2) {
-        if (w >= half && w < 2 * half) each(w - half, put);
-        __syncthreads();
-        if (w < half)
-            each(w, [&](const float4* d, int c, int j) {
-                const float4 v = *d;
-                o[c][j] += v.x; o[c][j + 1] += v.y; o[c][j + 2] += v.z; o[c][j + 3] += v.w;
-            });
-        __syncthreads();
-    }
-    if (w == 0) each(0, put);
+        for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<float4*>(lds + w * kPart + i * kOPitch + (32 * c + 8 * j + 4 * h) * 4) =
+                make_float4(o[c][4 * j], o[c][4 * j + 1], o[c][4 * j + 2], o[c][4 * j + 3]);
     __syncthreads();
     const size_t slot = ((static_cast<size_t>(b) * a.kv_heads + g) * a.splits + split) * nq;
-    if (threadIdx.x < kMxQ && qv < nq) {
-        if (a.splits > 1) a.ml[slot + qv] = make_float2(mt, lt);
-        else if (a.lse) a.lse[(static_cast<size_t>(b) * a.heads + head) * a.n_rows + row] = (mt + __log2f(lt)) * kLn2;
-    }
     for (int x = threadIdx.x; x < kMxQ * HD / 8; x += NW * kWave) {
-        const int r = x / (HD / 8), c = (x % (HD / 8)) * 8;
-        const int qx = qt * kMxQ + r;
+        const int rq = x / (HD / 8), c = (x % (HD / 8)) * 8;
+        const int qx = qt * kMxQ + rq;
         if (qx >= nq) continue;
-        const float4* s = reinterpret_cast<const float4*>(lds + r * kOPitch + 4 * c);
-        const float4 u = s[0], v = s[1];
+        float mt = -INFINITY, lt = 0.f, f[NW];
+#pragma unroll
+        for (int y = 0; y < NW; ++y) mt = fmaxf(mt, sm[y][rq]);
+        const float ref = mt == -INFINITY ? 0.f : mt;
+#pragma unroll
+        for (int y = 0; y < NW; ++y) {
+            f[y] = fast_exp2(sm[y][rq] - ref);
+            lt += sl[y][rq] * f[y];
+        }
+        float v[8] = {};
+#pragma unroll
+        for (int y = 0; y < NW; ++y) {
+            const float4* src = reinterpret_cast<const float4*>(lds + y * kPart + rq * kOPitch + 4 * c);
+            const float4 d = src[0], e = src[1];
+            v[0] = fmaf(d.x, f[y], v[0]); v[1] = fmaf(d.y, f[y], v[1]); v[2] = fmaf(d.z, f[y], v[2]); v[3] = fmaf(d.w, f[y], v[3]);
+            v[4] = fmaf(e.x, f[y], v[4]); v[5] = fmaf(e.y, f[y], v[5]); v[6] = fmaf(e.z, f[y], v[6]); v[7] = fmaf(e.w, f[y], v[7]);
+        }
+        const int hx = g * group + qx / a.n_rows, rx = qx % a.n_rows;
         if (a.splits > 1) {
             float4* d = reinterpret_cast<float4*>(a.part + (slot + qx) * HD + c);
-            d[0] = u;
-            d[1] = v;
+            d[0] = make_float4(v[0], v[1], v[2], v[3]);
+            d[1] = make_float4(v[4], v[5], v[6], v[7]);
+            if (c == 0) a.ml[slot + qx] = make_float2(mt, lt);
             continue;
         }
-        const size_t at = ((static_cast<size_t>(b) * a.n_rows + qx % a.n_rows) * a.heads + g * group + qx / a.n_rows) * HD + c;
+        // an empty sequence: zeros; no finite score: NaN, as the quotient
+        const float inv = len > 0 ? 1.f / lt : 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= inv;
+        const size_t at = ((static_cast<size_t>(b) * a.n_rows + rx) * a.heads + hx) * HD + c;
         if constexpr (BF16) {
-            st16(a.out + 2 * at, make_uint4(pack_bf16x2(u.x, u.y), pack_bf16x2(u.z, u.w), pack_bf16x2(v.x, v.y),
-                                            pack_bf16x2(v.z, v.w)));
+            st16(a.out + 2 * at, make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                            pack_bf16x2(v[6], v[7])));
         } else {
-            *reinterpret_cast<float4*>(a.out + 4 * at) = u;
-            *reinterpret_cast<float4*>(a.out + 4 * at + 16) = v;
+            *reinterpret_cast<float4*>(a.out + 4 * at) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4*>(a.out + 4 * at + 16) = make_float4(v[4], v[5], v[6], v[7]);
         }
+        if (a.lse && c == 0) a.lse[(static_cast<size_t>(b) * a.heads + hx) * a.n_rows + rx] = (mt + __log2f(lt)) * kLn2;
     }
 }
 
