@@ -801,7 +801,7 @@ def mx_store_kv(k: torch.Tensor, v: torch.Tensor, k_codes: torch.Tensor, k_scale
     if (idx is not None and idx.shape != (b, n)) or (count is not None and (idx is None or count.shape != (b,))):
         raise ValueError("mx_store_kv: idx must be [batch][n_rows], count [batch] and given with idx")
     rs = _mx_row_stride(k, "mx_store_kv")
-    if n * b > 1 and _mx_row_stride(v, "mx_store_kv") != rs:
+    if _mx_row_stride(v, "mx_store_kv") != rs:
         raise ValueError("mx_store_kv: k and v differ in row stride")
     dev = _mx_device(k, v, k_codes, k_scales, v_codes, v_scales, idx, count)
     _check("polestar_mx_store_kv", lib().polestar_mx_store_kv(

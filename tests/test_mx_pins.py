@@ -133,6 +133,17 @@ def test_workspace_sizes_of_bad_shapes_are_zero(L):
     assert ps.mx_attend_workspace_size(1, 1, 64, 4, 2, 96, 1) == 0
 
 
+def test_store_refuses_a_single_row_with_heads_out_of_order():
+    """One row has no row stride, but its heads still have to lie one after another, in v as in k."""
+    torch = pytest.importorskip("torch")
+    caches = [torch.zeros((1, 2, 9, n), dtype=torch.uint8) for n in (32, 2, 32, 2)]
+    good = torch.zeros(1, 1, 2, 64)
+    bad = torch.zeros(1, 1, 64, 2).transpose(2, 3)
+    for k, v in ((good, bad), (bad, good)):
+        with pytest.raises(ValueError, match="equally spaced"):
+            ps.mx_store_kv(k, v, *caches)
+
+
 def test_python_entry_points_refuse_cpu_tensors_and_shapes():
     torch = pytest.importorskip("torch")
     x = torch.zeros(2, 4, 64)
