@@ -12,7 +12,6 @@
 namespace ps {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool aligned_to(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 // Whether a caller's dtype argument names a supported type.  Taken by
 // reference and read as an int: a C caller may pass any int, and in C++

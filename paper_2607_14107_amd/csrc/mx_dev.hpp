@@ -16,6 +16,8 @@ namespace ps {
 
 constexpr int kMxBlock = 32;                     // channels per scale
 
+inline bool aligned_to(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef int intx2 __attribute__((ext_vector_type(2)));
 typedef short shortx2 __attribute__((ext_vector_type(2)));
