@@ -34,6 +34,7 @@ extern "C" {
  *   x : [batch][seq][n] dtype
  *   codes : out [batch][n_rows][row bytes];  scales : out [batch][n_rows][n / 32]
  * Weights are laid out by one call with batch 1, seq = n_rows = n_out.
+ * UNSUPPORTED above 65535 sequences or 2^35 channels of one sequence's rows.
  */
 polestar_status polestar_mx_quantize(int fmt, polestar_dtype dtype, int batch, int seq, int n, int row_start,
                                      int n_rows, const void* x, uint8_t* codes, uint8_t* scales,
@@ -43,7 +44,7 @@ polestar_status polestar_mx_quantize(int fmt, polestar_dtype dtype, int batch, i
  * polestar_mx_dequantize -- the values that codes and scales stand for, exact in
  * float and (but for magnitudes below 2^-126) in bf16.
  *   codes : [rows][row bytes];  scales : [rows][n / 32];  y : out [rows][n] dtype
- * rows >= 0 (0: nothing to do).
+ * rows >= 0 (0: nothing to do).  UNSUPPORTED above 2^35 channels.
  */
 polestar_status polestar_mx_dequantize(int fmt, polestar_dtype dtype, long rows, int n, const uint8_t* codes,
                                        const uint8_t* scales, void* y, hipStream_t stream);
@@ -61,8 +62,9 @@ polestar_status polestar_mx_dequantize(int fmt, polestar_dtype dtype, long rows,
  * bf16's, and fp32 outputs of MXFP8 rows are computed on bf16 matrix instructions
  * from the decoded values instead, with exact products.
  * A NaN block makes NaN of every output it takes part in.
- * UNSUPPORTED unless n_in % 128 == 0, n_out % 16 == 0 and codes, y and the
- * workspace are 16-byte aligned, scales 4-byte aligned.  rows >= 0.
+ * UNSUPPORTED unless n_in % 128 == 0, n_out % 16 == 0, both at most 2^22, rows at
+ * most 2^24, and codes, y and the workspace are 16-byte aligned, scales 4-byte
+ * aligned.  rows >= 0.
  */
 size_t polestar_mx_linear_workspace_size(int x_fmt, polestar_dtype dtype, long rows, int n_out, int n_in);
 polestar_status polestar_mx_linear(int x_fmt, polestar_dtype dtype, long rows, int n_in, int n_out,
@@ -95,8 +97,8 @@ polestar_status polestar_mx_quantize_linear(int x_fmt, polestar_dtype dtype, int
  *   gain : [d] float, or NULL (unit gain)
  *   x_out : out [rows][d] float, may be x; may be NULL where y is NULL
  *   codes : out [rows][row bytes];  scales : out [rows][d / 32]
- * UNSUPPORTED unless d % 32 == 0, d <= 16384 and every pointer but scales is
- * 16-byte aligned.  rows >= 0.
+ * UNSUPPORTED unless d % 32 == 0, d <= 16384, rows < 2^24 and every pointer but
+ * scales is 16-byte aligned.  rows >= 0.
  */
 polestar_status polestar_residual_rmsnorm_mx(int fmt, polestar_dtype dtype, long rows, int d, const float* x,
                                              const void* y, const float* gain, float eps, float* x_out,
@@ -120,9 +122,9 @@ polestar_status polestar_residual_rmsnorm_mx(int fmt, polestar_dtype dtype, long
  *   idx : [batch][n_rows] int32 or NULL;  count : [batch] int32, clamped to
  *         [0, n_rows] (NULL with idx: n_rows)
  * Requires 0 <= n_rows, row_start + n_rows <= seq without idx, row_stride >=
- * n_kv_heads * head_dim.  UNSUPPORTED unless head_dim is 64 or 128, a stride is
- * a whole number of 16-byte chunks, and k, v and the codes are 16-byte, the
- * scales 4-byte aligned (head_dim 64: 2-byte).
+ * n_kv_heads * head_dim.  UNSUPPORTED unless head_dim is 64 or 128, n_rows <
+ * 2^24, batch < 2^16, a stride is a whole number of 16-byte chunks, and k, v and
+ * the codes are 16-byte, the scales 4-byte aligned (head_dim 64: 2-byte).
  */
 polestar_status polestar_mx_store_kv(polestar_dtype dtype, int batch, int seq, int n_kv_heads, int head_dim,
                                      int n_rows, const void* k, const void* v, long row_stride,
@@ -147,9 +149,10 @@ polestar_status polestar_mx_store_kv(polestar_dtype dtype, int batch, int seq, i
  * probabilities are rounded to bf16 for bf16 outputs, and for fp32 queries both
  * they and the probabilities are taken as three bf16 terms (24 bits).
  * UNSUPPORTED unless head_dim is 64 or 128, n_heads % n_kv_heads == 0 is given
- * (INVALID otherwise), q_stride is a whole number of 16-byte chunks, and q, out,
- * the codes and the workspace are 16-byte, the scales 4-byte aligned (head_dim
- * 64: 2-byte).
+ * (INVALID otherwise), seq <= 2^24, batch and n_kv_heads < 2^16, the query heads'
+ * rows fit 2^23 groups of 32 in all, q_stride is a whole number of 16-byte chunks,
+ * and q, out, the codes and the workspace are 16-byte, the scales 4-byte aligned
+ * (head_dim 64: 2-byte).
  */
 size_t polestar_mx_attend_workspace_size(polestar_dtype dtype, int batch, int seq, int n_heads, int n_kv_heads,
                                          int head_dim, int n_rows);
