@@ -84,7 +84,7 @@ constexpr int kMxTileThreads = 512;                      // eight waves, two per
 constexpr int kMxBand = 4;                               // row tiles per band of the launch order
 constexpr int kMxCus = 256;
 
-// Transfers into LDS, 16 or 12 bytes per lane, from a buffer of `bytes` bytes at base: a
+// Transfers into LDS, 16 bytes per lane, from a buffer of `bytes` bytes at base: a
 // lane's offset is one register, the K tile's a scalar; the lanes land one after
 // another from lds on.  Written out, because the compiler waits for every transfer
 // that it knows of before it reads LDS; the waits are the kernel's own (mx_wait_vm
@@ -104,9 +104,6 @@ __device__ __forceinline__ uint32_t lds_offset(const char* p) {
 __device__ __forceinline__ void mx_dma16(MxBuffer b, uint32_t lane_off, uint32_t off, const char* lds) {
     PS_MX_DMA("buffer_load_dwordx4");
 }
-__device__ __forceinline__ void mx_dma12(MxBuffer b, uint32_t lane_off, uint32_t off, const char* lds) {
-    PS_MX_DMA("buffer_load_dwordx3");
-}
 #undef PS_MX_DMA
 // s_waitcnt immediates: at most n vector-memory operations outstanding / LDS reads done
 constexpr int mx_wait_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
@@ -122,10 +119,10 @@ template <int FMT_, int WM_, int MI_, int NJ_, int KS_> struct MxShape {
     // LDS: slots of a K tile's codes, as many as fit, beside two buffers of the
     // scales of a round of K tiles
     static constexpr int kX = BM * X::kBytes, kSlot = kX + BN * W::kBytes, kLds = 160 * 1024;
-    static constexpr bool fits(int ns) { return ns * kSlot + 2 * 4 * ns * KS * (BM + BN) <= kLds; }
+    static constexpr int kRow = 16, kScales = kRow * (BM + BN);   // a row's scales of a round, four steps at most
+    static constexpr bool fits(int ns) { return ns * kSlot + 2 * kScales <= kLds; }
     static constexpr int NS = fits(4) ? 4 : fits(3) ? 3 : 2;
-    static constexpr int kRow = 4 * NS * KS, kScales = kRow * (BM + BN);   // a row's scales of a round
-    static_assert(fits(NS) && (kRow == 12 || kRow == 16), "");
+    static_assert(fits(NS) && 4 * NS * KS <= kRow, "");
 };
 
 // Workgroup blk -> (split, row tile, column tile): consecutive workgroups go to
@@ -189,8 +186,7 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
                                : mx_buffer(g.ws + static_cast<size_t>(n0) * srow, nrows * srow);
     const uint32_t ssrc = static_cast<uint32_t>(of_x ? 64 * sg + lane : 64 * sg + lane - BM) * srow;
     auto issue_scales = [&](int t, int buf) {
-        if constexpr (T::kRow == 16) mx_dma16(sbuf, ssrc, 4 * (q0 + t * KS), sc + buf + 64 * T::kRow * sg);
-        else mx_dma12(sbuf, ssrc, 4 * (q0 + t * KS), sc + buf + 64 * T::kRow * sg);
+        mx_dma16(sbuf, ssrc, 4 * (q0 + t * KS), sc + buf + 64 * T::kRow * sg);
     };
     // DMA instructions d0 .. d0 + n - 1 of K tile t (past the split: its last one again)
     auto issue = [&](int d0, int n, int t, const char* slot) {

@@ -207,6 +207,31 @@ def test_linear_matches_the_oracle(P, fmt, dtype, rows, n_in, n_out):
     _guards_hold(buf)
 
 
+LARGE = [(4096, 384, 4096), (4000, 128, 4112), (2048, 896, 4096), (1000, 1152, 4096), (8192, 640, 2064), (1500, 2176, 4608),
+         (512, 4224, 4096), (500, 2688, 2064)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("fmt", ["mxfp4", "mxfp8"])
+@pytest.mark.parametrize("rows,n_in,n_out", LARGE)
+def test_linear_of_many_tiles_matches_the_oracle(P, fmt, dtype, rows, n_in, n_out):
+    """Products that fill the GPU, on the larger tiles: 64 rows and 64 outputs of them are checked."""
+    torch = _torch()
+    g = np.random.default_rng(rows + n_in)
+    xc, xs, x = _held(g, (rows, n_in), fmt)
+    wc, wsc, w = _held(g, (n_out, n_in), "mxfp4")
+    y = torch.empty((rows, n_out), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    P.mx_linear(P.CODECS[fmt], _dev(xc), _dev(xs), _dev(wc), _dev(wsc), y)
+    r = np.unique(np.concatenate((g.integers(0, rows, 62), [0, rows - 1])))
+    c = np.unique(np.concatenate((g.integers(0, n_out, 62), [0, n_out - 1])))
+    got = y.double().cpu().numpy()
+    for rr, cc in ((r, slice(None)), (slice(None), c)):
+        want = x[rr] @ w[cc].T
+        err = np.abs(got[rr][:, cc] - want)
+        tol = _linear_bound(x[rr], w[cc], want, fmt, dtype)
+        assert (err <= tol).all(), (err / tol).max()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("fmt", ["mxfp4", "mxfp8"])
 @pytest.mark.parametrize("rows", [3, 40, 200])
