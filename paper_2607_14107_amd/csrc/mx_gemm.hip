@@ -14,6 +14,7 @@
 // to fp32.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "host_common.hpp"
 #include "mx_dev.hpp"
@@ -98,32 +99,42 @@ __device__ __forceinline__ MxBuffer mx_buffer(const void* base, uint32_t bytes) 
 __device__ __forceinline__ uint32_t lds_offset(const char* p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
 }
-#define PS_MX_DMA(OP)                                                                      \
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t" OP " %1, %2, %3 offen lds"             \
-                 :: "s"(uniform(lds_offset(lds))), "v"(lane_off), "s"(b), "s"(uniform(off)) : "memory")
 __device__ __forceinline__ void mx_dma16(MxBuffer b, uint32_t lane_off, uint32_t off, const char* lds) {
-    PS_MX_DMA("buffer_load_dwordx4");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :: "s"(uniform(lds_offset(lds))), "v"(lane_off), "s"(b), "s"(uniform(off)) : "memory");
 }
-#undef PS_MX_DMA
 // s_waitcnt immediates: at most n vector-memory operations outstanding / LDS reads done
 constexpr int mx_wait_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
 constexpr int kMxWaitLgkm0 = 15 | (3 << 14) | (7 << 4);
 
 // A tile shape: BM = 16 MI WM rows x BN = 16 NJ (8 / WM) outputs per workgroup, its
-// eight waves in a WM x (8 / WM) grid of MI x NJ tiles; K tiles of KS steps.
-template <int FMT_, int WM_, int MI_, int NJ_, int KS_> struct MxShape {
-    static constexpr int FMT = FMT_, WM = WM_, WN = 8 / WM_, MI = MI_, NJ = NJ_, KS = KS_;
+// eight waves in a WM x (8 / WM) grid of MI x NJ tiles; K tiles of KS steps, NS of them
+// in LDS; scales for R steps at a time, in two buffers.
+template <int FMT_, int WM_, int MI_, int NJ_, int KS_, int NS_, int R_> struct MxShape {
+    static constexpr int FMT = FMT_, WM = WM_, WN = 8 / WM_, MI = MI_, NJ = NJ_, KS = KS_, NS = NS_, R = R_;
     static constexpr int BM = 16 * MI * WM, BN = 16 * NJ * WN;
-    using X = LdsRow<FMT, KS>;
+    // (the rows' steps one after another where two are more than an LDS row)
+    static constexpr int kPlanes = FMT == POLESTAR_MXFP8 ? KS : 1;
+    using X = LdsRow<FMT, KS / kPlanes>;
     using W = LdsRow<POLESTAR_MXFP4, KS>;
-    // LDS: slots of a K tile's codes, as many as fit, beside two buffers of the
-    // scales of a round of K tiles
-    static constexpr int kX = BM * X::kBytes, kSlot = kX + BN * W::kBytes, kLds = 160 * 1024;
-    static constexpr int kRow = 16, kScales = kRow * (BM + BN);   // a row's scales of a round, four steps at most
-    static constexpr bool fits(int ns) { return ns * kSlot + 2 * kScales <= kLds; }
-    static constexpr int NS = fits(4) ? 4 : fits(3) ? 3 : 2;
-    static_assert(fits(NS) && 4 * NS * KS <= kRow, "");
+    static constexpr int kPlane = BM * X::kBytes, kX = kPlanes * kPlane, kSlot = kX + BN * W::kBytes;
+    // a row's scales of R steps: chunks of 16 bytes, a lane each, swizzled like the
+    // codes' (16 rows' reads in different banks)
+    static constexpr int kChunks = (R + 3) / 4, kRow = 16 * kChunks, kScales = kRow * (BM + BN);
+    static constexpr int kSRows = 64 / kChunks;          // rows of a transfer
+    __device__ __forceinline__ static int scale_chunk(int row, int c) { return (c ^ row / (16 / kChunks) % kChunks) << 4; }
+    static constexpr int kUnroll = R / KS;               // K tiles
+    static_assert(NS * kSlot + 2 * kScales <= 160 * 1024 && kUnroll % NS == 0 && R % KS == 0, "");
 };
+
+// The scales of step `step` of the round in the buffer at byte buf.
+struct Scales {
+    int buf, step;
+};
+
+template <class F, int... U> __device__ __forceinline__ void mx_unrolled(F f, std::integer_sequence<int, U...>) {
+    (f(std::integral_constant<int, U>{}), ...);
+}
 
 // Workgroup blk -> (split, row tile, column tile): consecutive workgroups go to
 // different XCDs, so the ids are first regrouped per XCD, and each XCD walks
@@ -144,15 +155,25 @@ __device__ __forceinline__ void mx_tile_coords(const MxGemmArgs& g, int blk, int
 
 // A workgroup's tile: codes and scales by DMA into LDS slots, one barrier per K tile,
 // a wave's blocks on the 16x16x128 scaled instruction (DEC: four 16x16x32 bf16 ones).
+//
+// What bounds it.  The DMA costs by the cache line, whatever is read of it (2 to 3
+// clocks each and a compute unit's 64 bytes per clock at most): K tiles of whole lines
+// and scales of 16 steps at a time took 512 x 12288 x 4096 from 36.3 to 28.3 us (MXFP8,
+// 1.8 PFLOP/s) and 33.1 to 21.3 (MXFP4, 2.4); there the transfers alone take 23 us, the
+// reads and products alone 24; more slots (8 K tiles in flight) gained nothing, nor did
+// two groups of waves with a step each (a third fewer LDS reads).  The large tiles are
+// bound by power: 12288 x 4096 x 24576 takes 0.92 to 0.96 ms (MXFP8, 2.6 PFLOP/s) and
+// 0.62 (MXFP4, 4.0) at 1.7 and 1.85 GHz with the matrix units 65 and 44% busy.
 template <class T, bool BF16>
 __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     constexpr int FMT = T::FMT, MI = T::MI, NJ = T::NJ, KS = T::KS, BM = T::BM, BN = T::BN, NS = T::NS;
     constexpr bool DEC = FMT == POLESTAR_MXFP8 && !BF16;
     constexpr int XB = T::X::kBytes, WB = T::W::kBytes;
-    constexpr int XG = BM * XB / 1024, WG = BN * WB / 1024, SG = (BM + BN) / 64;   // DMA groups of a K tile
-    constexpr int XI = (XG + 7) / 8, WI = (WG + 7) / 8;  // instructions per wave
+    constexpr int XG = BM * XB / 1024, WG = BN * WB / 1024;   // DMA groups of a K tile
+    constexpr int XI = (XG * T::kPlanes + 7) / 8, WI = (WG + 7) / 8;   // instructions per wave
+    static_assert(T::kPlanes == 1 || XG % 8 == 0, "");
     constexpr int ND = XI + WI;
-    static_assert(SG <= 8, "a wave per group of scales");
+    constexpr int SXG = BM / T::kSRows, SG = SXG + BN / T::kSRows, SI = (SG + 7) / 8;   // of R steps' scales
     __shared__ __align__(16) char lds[NS * T::kSlot + 2 * T::kScales];
     char* const sc = lds + NS * T::kSlot;
 
@@ -178,22 +199,23 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     const int xg = min(w, XG - 1), wg = min(w, WG - 1), xr = xg * XR + lane / (XB / 16), wr = wg * WR + lane / (WB / 16);
     const uint32_t xsrc = xr * xrow + T::X::chunk(xr, lane % (XB / 16));   // (the swizzle repeats with the groups)
     const uint32_t wsrc = wr * wrow + T::W::chunk(wr, lane % (WB / 16));
-    // Scales, a round of NS K tiles at a time, 64 rows of x or of w per wave.  (A step's
-    // four bytes at a time are a cache line each too, and took a quarter of the time.)
-    const int sg = min(w, SG - 1);
-    const bool of_x = sg < BM / 64;
-    const MxBuffer sbuf = of_x ? mx_buffer(g.xs + static_cast<size_t>(m0) * srow, mrows * srow)
-                               : mx_buffer(g.ws + static_cast<size_t>(n0) * srow, nrows * srow);
-    const uint32_t ssrc = static_cast<uint32_t>(of_x ? 64 * sg + lane : 64 * sg + lane - BM) * srow;
+    // Scales, R steps at a time: a row's are one cache line for 32 steps.
+    const MxBuffer xsbuf = mx_buffer(g.xs + static_cast<size_t>(m0) * srow, mrows * srow);
+    const MxBuffer wsbuf = mx_buffer(g.ws + static_cast<size_t>(n0) * srow, nrows * srow);
     auto issue_scales = [&](int t, int buf) {
-        mx_dma16(sbuf, ssrc, 4 * (q0 + t * KS), sc + buf + 64 * T::kRow * sg);
+#pragma unroll
+        for (int d = 0; d < SI; ++d) {
+            const int gr = min(w + 8 * d, SG - 1), row = (gr < SXG ? gr : gr - SXG) * T::kSRows + lane / T::kChunks;
+            mx_dma16(gr < SXG ? xsbuf : wsbuf, row * srow + T::scale_chunk(row, lane % T::kChunks), 4 * (q0 + t * KS),
+                     sc + buf + gr * T::kSRows * T::kRow);
+        }
     };
     // DMA instructions d0 .. d0 + n - 1 of K tile t (past the split: its last one again)
     auto issue = [&](int d0, int n, int t, const char* slot) {
-        const uint32_t k = min(t, nkt - 1), kx = q0 * (XB / KS) + k * XB, kw = q0 * (WB / KS) + k * WB;
+        const uint32_t k = q0 + min(t, nkt - 1) * KS, kx = k * (16 * Mx<FMT>::kBits), kw = k * 64;
 #pragma unroll
         for (int d = d0; d < d0 + n; ++d) {
-            if (d < XI) mx_dma16(xbuf, xsrc, kx + 8 * d * XR * xrow, slot + (xg + 8 * d) * 1024);
+            if (d < XI) mx_dma16(xbuf, xsrc, kx + 8 * d % max(XG, 8) * XR * xrow + 8 * d / max(XG, 8) * XB, slot + (xg + 8 * d) * 1024);
             else if (d < ND)
                 mx_dma16(wbuf, wsrc, kw + 8 * (d - XI) * WR * wrow, slot + T::kX + (wg + 8 * (d - XI)) * 1024);
         }
@@ -208,16 +230,17 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     Frag<FMT, DEC> fx[SETS][NX];
     Frag<POLESTAR_MXFP4, DEC> fw[SETS][NW];
     uint32_t sx[SETS][NX], sw[SETS][NW];                 // scale bytes
-    const char* const xsc = sc + (16 * MI * wm + r) * T::kRow + grp;
-    const char* const wsc = sc + (BM + 16 * NJ * wn + r) * T::kRow + grp;
-    // fragment j of step s of a slot, its scales at o in the buffers
-    auto read_x = [&](int set, int j, const char* slot, int s, int o) {
-        T::X::load(fx[set][j % NX], slot + 16 * (MI * wm + j) * XB, r, s, grp);
-        sx[set][j % NX] = *reinterpret_cast<const uint8_t*>(xsc + o + 16 * T::kRow * j);
+    // a step's scales in the buffers: of row `row`, which is r behind a tile's first
+    auto scales_at = [&](int row, int step) { return row * T::kRow + T::scale_chunk(r, step / 4) + 4 * (step % 4) + grp; };
+    // fragment j of step s of a slot, its scales those of step `q` of a round
+    auto read_x = [&](int set, int j, const char* slot, int s, Scales q) {
+        const int plane = T::kPlanes > 1 ? s * T::kPlane : 0;
+        T::X::load(fx[set][j % NX], slot + plane + 16 * (MI * wm + j) * XB, r, s, grp);
+        sx[set][j % NX] = *reinterpret_cast<const uint8_t*>(sc + q.buf + scales_at(16 * MI * wm + r, q.step) + 16 * T::kRow * j);
     };
-    auto read_w = [&](int set, int j, const char* slot, int s, int o) {
+    auto read_w = [&](int set, int j, const char* slot, int s, Scales q) {
         T::W::load(fw[set][j % NW], slot + T::kX + 16 * (NJ * wn + j) * WB, r, s, grp);
-        sw[set][j % NW] = *reinterpret_cast<const uint8_t*>(wsc + o + 16 * T::kRow * j);
+        sw[set][j % NW] = *reinterpret_cast<const uint8_t*>(sc + q.buf + scales_at(BM + 16 * NJ * wn + r, q.step) + 16 * T::kRow * j);
     };
     floatx4 acc[MI][NJ];
 #pragma unroll
@@ -260,34 +283,31 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     // barrier, 8% slower.)
     auto slot_of = [&](int u) { return lds + u % NS * T::kSlot; };
     auto scales_of = [&](int step, int buf) {            // of a step of this round, or the next round's first
-        return step < NS * KS ? buf + 4 * step : buf ^ T::kScales;
+        return step < T::R ? Scales{buf, step} : Scales{buf ^ T::kScales, 0};
     };
     int buf = 0, t = 0;
     auto rounds = [&](int whole, auto ktile) {           // K tiles 0 .. whole - 1
-        using std::integral_constant;
-        for (; t + NS <= whole; t += NS, buf ^= T::kScales) {
-            ktile(t, integral_constant<int, 0>{});
-            issue_scales(t + NS, buf ^ T::kScales);      // landed by the last sync of this round
-            ktile(t + 1, integral_constant<int, 1>{});
-            if constexpr (NS > 2) ktile(t + 2, integral_constant<int, 2>{});
-            if constexpr (NS > 3) ktile(t + 3, integral_constant<int, 3>{});
-        }
-        if (t < whole) ktile(t, integral_constant<int, 0>{});
-        if (NS > 2 && t + 1 < whole) ktile(t + 1, integral_constant<int, 1>{});
-        if constexpr (NS > 3)
-            if (t + 2 < whole) ktile(t + 2, integral_constant<int, 2>{});
+        constexpr int kUnroll = T::kUnroll;
+        for (; t + kUnroll <= whole; t += kUnroll, buf ^= T::kScales)
+            mx_unrolled([&](auto u) {
+                ktile(t + u, u);
+                if (u == 0) issue_scales(t + kUnroll, buf ^ T::kScales);   // landed by the last sync of this round
+            }, std::make_integer_sequence<int, kUnroll>{});
+        mx_unrolled([&](auto u) {
+            if (t + u < whole) ktile(t + u, u);
+        }, std::make_integer_sequence<int, kUnroll - 1>{});
     };
     if constexpr (kRing) {
         constexpr int NI = 4;                            // tiles of the operand that is held
-        auto read_ring = [&](int j, const char* slot, int s, int o) {
-            if constexpr (kRingX) read_x(0, j, slot, s, o);
-            else read_w(0, j, slot, s, o);
+        auto read_ring = [&](int j, const char* slot, int s, Scales q) {
+            if constexpr (kRingX) read_x(0, j, slot, s, q);
+            else read_w(0, j, slot, s, q);
         };
-        auto read_held = [&](int set, const char* slot, int s, int o) {
+        auto read_held = [&](int set, const char* slot, int s, Scales q) {
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                if constexpr (kRingX) read_w(set, j, slot, s, o);
-                else read_x(set, j, slot, s, o);
+                if constexpr (kRingX) read_w(set, j, slot, s, q);
+                else read_x(set, j, slot, s, q);
             }
         };
         auto row = [&](int j) {
@@ -297,16 +317,16 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
                 else mma(0, 0, i, j);
             }
         };
-        read_held(0, lds, 0, 0);
+        read_held(0, lds, 0, Scales{0, 0});
 #pragma unroll
-        for (int j = 0; j < 4; ++j) read_ring(j, lds, 0, 0);
+        for (int j = 0; j < 4; ++j) read_ring(j, lds, 0, Scales{0, 0});
         constexpr int DPR = (ND + 2) / 3;                // DMA instructions behind each of the last three
         auto ktile = [&](int kt, auto which) {
             constexpr int U = decltype(which)::value;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const bool last = s == KS - 1;
-                const int o = scales_of(U * KS + s, buf), on = scales_of(U * KS + s + 1, buf);
+                const Scales q = scales_of(U * KS + s, buf), qn = scales_of(U * KS + s + 1, buf);
                 const char* next = last ? slot_of(U + 1) : slot_of(U);
                 const int sn = last ? 0 : s + 1;
 #pragma unroll
@@ -314,11 +334,11 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
                     row(j);
                     if (j == 4) {
                         if (last) sync();
-                        read_held(1, next, sn, on);
+                        read_held(1, next, sn, qn);
                     }
                     fence();
-                    if (j < 4) read_ring(j + 4, slot_of(U), s, o);
-                    else read_ring(j - 4, next, sn, on);
+                    if (j < 4) read_ring(j + 4, slot_of(U), s, q);
+                    else read_ring(j - 4, next, sn, qn);
                     if (last && j > 4) issue((j - 5) * DPR, DPR, kt + NS, slot_of(U));
                     fence();
                 }
@@ -341,32 +361,44 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 row(j);
-                if (j < 4) read_ring(j + 4, lds + u * T::kSlot, 0, buf + 4 * u * KS);
+                if (j < 4) read_ring(j + 4, slot_of(u), 0, scales_of(u * KS, buf));
             }
         }
     } else {
-        static_assert(KS == 1 && NS % 2 == 0, "two register sets, in turn");
+        static_assert(T::R % 2 == 0, "two register sets, in turn");
         constexpr int DPR = (ND + MI - 1) / MI;
-        auto read = [&](int set, const char* slot, int o) {
+        auto read = [&](int set, const char* slot, int s, Scales q) {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) read_w(set, j, slot, 0, o);
+            for (int j = 0; j < NJ; ++j) read_w(set, j, slot, s, q);
 #pragma unroll
-            for (int j = 0; j < MI; ++j) read_x(set, j, slot, 0, o);
+            for (int j = 0; j < MI; ++j) read_x(set, j, slot, s, q);
         };
-        read(0, lds, 0);
-        rounds(nkt, [&](int kt, auto which) {
-            constexpr int U = decltype(which)::value, S = U % 2;
-            sync();
-            read(1 - S, slot_of(U + 1), scales_of(U + 1, buf));
-            fence();
+        read(0, lds, 0, Scales{0, 0});
+        const int whole = nst / KS;
+        rounds(whole, [&](int kt, auto which) {
+            constexpr int U = decltype(which)::value;
 #pragma unroll
-            for (int a = 0; a < MI; ++a) {
-#pragma unroll
-                for (int b = 0; b < NJ; ++b) mma(S, S, a, b);
-                issue(a * DPR, DPR, kt + NS, slot_of(U));
+            for (int s = 0; s < KS; ++s) {
+                const bool last = s == KS - 1;
+                const int set = (U * KS + s) % 2;
+                if (last) sync();
+                read(1 - set, last ? slot_of(U + 1) : slot_of(U), last ? 0 : s + 1, scales_of(U * KS + s + 1, buf));
                 fence();
+#pragma unroll
+                for (int a = 0; a < MI; ++a) {
+#pragma unroll
+                    for (int b = 0; b < NJ; ++b) mma(set, set, a, b);
+                    if (last) issue(a * DPR, DPR, kt + NS, slot_of(U));
+                    fence();
+                }
             }
         });
+        if (KS > 1 && whole < nkt) {                     // one step is left
+#pragma unroll
+            for (int a = 0; a < MI; ++a)
+#pragma unroll
+                for (int b = 0; b < NJ; ++b) mma(0, 0, a, b);
+        }
     }
     __builtin_amdgcn_s_waitcnt(0);                       // every DMA (the re-read tail too) has landed
     __syncthreads();                                     // and every wave is done with the slots
@@ -634,19 +666,36 @@ __global__ __launch_bounds__(256) void mx_reduce_kernel(const float* __restrict_
     else reinterpret_cast<float4*>(y)[i] = v;
 }
 
-// The tile shapes by rows and outputs.  MXFP8 rows: a wave's block is half as wide in
-// rows, whose fragments are twice the bytes.  The decoding form has no registers for
-// the two largest.
-constexpr bool mx_has_tile(int fmt, bool bf16, int bm, int bn) { return bm * bn < 256 * 128 || fmt == POLESTAR_MXFP4 || bf16; }
+// The tile shapes by rows and outputs.  A wave's block has four of its 16 x 16 tiles on
+// one side at least, rows or outputs by which fragments are fewer bytes, and K tiles of
+// 256 channels (whole cache lines of the weights) where LDS holds enough of them:
+// MXFP8, 64 x 128: 36.3 -> 31.2 us for 512 x 12288 x 4096; 128 x 128 and 128 x 256 with
+// two of 256 instead of four of 128 channels were 0 to 16% slower.
 template <int FMT, int BM, int BN> struct ShapeOf;
-template <> struct ShapeOf<POLESTAR_MXFP8, 256, 256> { using T = MxShape<POLESTAR_MXFP8, 2, 8, 4, 1>; };
-template <> struct ShapeOf<POLESTAR_MXFP4, 256, 256> { using T = MxShape<POLESTAR_MXFP4, 2, 8, 4, 2>; };
-template <int FMT> struct ShapeOf<FMT, 128, 256> { using T = MxShape<FMT, 2, 4, 4, 1>; };
-template <> struct ShapeOf<POLESTAR_MXFP8, 128, 128> { using T = MxShape<POLESTAR_MXFP8, 4, 2, 4, 1>; };
-template <> struct ShapeOf<POLESTAR_MXFP4, 128, 128> { using T = MxShape<POLESTAR_MXFP4, 2, 4, 2, 1>; };
-template <int FMT> struct ShapeOf<FMT, 64, 256> { using T = MxShape<FMT, 2, 2, 4, 1>; };
-template <int FMT> struct ShapeOf<FMT, 64, 128> { using T = MxShape<FMT, 2, 2, 2, 1>; };
+template <> struct ShapeOf<POLESTAR_MXFP8, 256, 256> { using T = MxShape<POLESTAR_MXFP8, 2, 8, 4, 1, 3, 3>; };
+template <> struct ShapeOf<POLESTAR_MXFP4, 256, 256> { using T = MxShape<POLESTAR_MXFP4, 2, 8, 4, 2, 2, 4>; };
+template <> struct ShapeOf<POLESTAR_MXFP8, 128, 256> { using T = MxShape<POLESTAR_MXFP8, 2, 4, 4, 1, 4, 8>; };
+template <> struct ShapeOf<POLESTAR_MXFP4, 128, 256> { using T = MxShape<POLESTAR_MXFP4, 2, 4, 4, 2, 2, 16>; };
+template <> struct ShapeOf<POLESTAR_MXFP8, 128, 128> { using T = MxShape<POLESTAR_MXFP8, 4, 2, 4, 1, 4, 16>; };
+template <> struct ShapeOf<POLESTAR_MXFP4, 128, 128> { using T = MxShape<POLESTAR_MXFP4, 2, 4, 2, 2, 4, 16>; };
+template <> struct ShapeOf<POLESTAR_MXFP8, 64, 256> { using T = MxShape<POLESTAR_MXFP8, 2, 2, 4, 1, 4, 16>; };
+template <int FMT> struct ShapeOf<FMT, 64, 128> { using T = MxShape<FMT, 2, 2, 2, 2, 4, 16>; };
 #define PS_MX_SHAPES(X) X(256, 256) X(128, 256) X(128, 128) X(64, 256) X(64, 128)
+
+// A shape's time per step (us) for MXFP8 rows, MXFP4 rows and the decoded form; 0: not
+// used there.  (The decoded form has no registers for the two largest; 64 x 256 in the
+// others and 128 x 128 in the decoded form gained 0.1% in the mean.)
+constexpr struct MxStep {
+    int bm, bn;
+    double us[3];
+} kMxSteps[] = {{256, 256, {1.57, 1.26, 0}}, {128, 256, {0.82, 0.63, 0}}, {128, 128, {0.50, 0.41, 0}},
+                {64, 256, {0, 0, 0.69}}, {64, 128, {0.29, 0.23, 0.40}}};
+constexpr int mx_class(int x_fmt, bool bf16) { return x_fmt == POLESTAR_MXFP4 ? 1 : bf16 ? 0 : 2; }
+constexpr bool mx_has_tile(int x_fmt, bool bf16, int bm, int bn) {
+    for (const auto& s : kMxSteps)
+        if (s.bm == bm && s.bn == bn) return s.us[mx_class(x_fmt, bf16)] > 0;
+    return false;
+}
 
 struct MxPlan {
     int bm, bn, ksplit, steps;
@@ -655,29 +704,28 @@ struct MxPlan {
 
 // Tile shape and K split with the least estimated time (us): rounds of one workgroup
 // per CU, each its steps and a fixed cost, and for a split the reduction's launch and
-// the partials' way through memory (per MB).  Measured over 4276 random shapes of 17
-// to 8192 rows, 128 to 24576 outputs and 256 to 12288 channels with every shape and
-// split: the plan that these constants choose is 1.3% (MXFP8), 1.9% (MXFP4) and 0.6%
-// (decoded) slower than the fastest in the geometric mean, 9, 11 and 4% at the 95th
-// percentile, 44% at most.
+// the partials' way through memory (per MB).  The constants are fitted to half of 8197
+// random shapes of 17 to 8192 rows, 128 to 24576 outputs and 256 to 12288 channels,
+// each with every tile shape and split: on the other half the chosen plan is 1.0%
+// (MXFP8), 1.3% (MXFP4) and 0.6% (decoded) slower than the fastest in the geometric
+// mean, 7, 9 and 6% at the 95th percentile, 30% at most.
 MxPlan mx_plan(int x_fmt, bool bf16, long rows, int n_out, int n_in) {
-    const bool dec = x_fmt == POLESTAR_MXFP8 && !bf16;
-    static constexpr struct { int bm, bn; double step, decoded; } shapes[] = {
-        {256, 256, 1.5, 0}, {128, 256, 0.9, 0}, {128, 128, 0.55, 0.75}, {64, 256, 0.6, 0.65}, {64, 128, 0.36, 0.39}};
-    const double fixed = dec ? 3.0 : 4.0, launch = dec ? 2.0 : 4.0, per_mb = dec ? 0.31 : 0.4;
+    static constexpr struct { double fixed, launch, per_mb; } costs[] = {{3.2, 2.9, 1.2}, {2.5, 3.75, 1.0}, {3.5, 1.5, 0.47}};
+    const int cls = mx_class(x_fmt, bf16);
+    const auto& c = costs[cls];
     const int nst = n_in / 128;
     MxPlan p{};
     double best = 1e30;
-    for (const auto& s : shapes) {
-        if (!mx_has_tile(x_fmt, bf16, s.bm, s.bn)) continue;
+    for (const auto& s : kMxSteps) {
+        if (s.us[cls] == 0) continue;
         const long tiles = (rows + s.bm - 1) / s.bm * ceil_div(n_out, s.bn);
         for (int ks = 1; ks <= 16 && ks <= nst; ++ks) {
-            const int steps = ceil_div(ceil_div(nst, ks), 2) * 2;   // whole K tiles of every shape
+            const int steps = ceil_div(ceil_div(nst, ks), 2) * 2;   // whole K tiles
             if (ceil_div(nst, steps) != ks) continue;
             if (ks > 1 && (tiles * (ks - 1) >= kMxCus || steps < 4)) break;
             const double rounds = static_cast<double>((tiles * ks + kMxCus - 1) / kMxCus);
-            const double cost = rounds * (std::min(steps, nst) * (dec ? s.decoded : s.step) + fixed) +
-                                (ks > 1 ? launch + 4.0 * ks * rows * n_out * 1e-6 * per_mb : 0.0);
+            const double cost = rounds * (std::min(steps, nst) * s.us[cls] + c.fixed) +
+                                (ks > 1 ? c.launch + 4.0 * ks * rows * n_out * 1e-6 * c.per_mb : 0.0);
             if (cost < best) {
                 best = cost;
                 p = MxPlan{s.bm, s.bn, ks, steps, ks > 1 ? 4 * static_cast<size_t>(ks) * rows * n_out : 0};
@@ -706,15 +754,19 @@ void mx_launch_few(const MxFewArgs& g, int nt, hipStream_t stream) {
 // workgroups per compute unit.
 int mx_few_nt(int n_out) { return ceil_div(n_out, 16) > 2 * kMxCus ? 2 : 1; }
 
-// Whether the few-rows kernels take a product: where the rows' codes, which every
-// workgroup reads again, are at most 34 MB in all.  Against the tile kernel's best
-// plan, us: 4096 x 4096, MXFP8, 1 row 3.5 (7.1), 16 rows (17 MB) 5.1 (7.7), 32 rows
-// (34 MB) 7.2 (8.7), 64 rows (67 MB) 11.3 (10.3); 12288 x 4096, 1 row (2 MB) 8.3
-// (9.8), 16 rows (25 MB) 11.1 (10.5), 32 rows (50 MB) 16.2 (11.7).
+// Whether the few-rows kernels take a product: where the rows' codes that a compute
+// unit reads, once per workgroup, are at most 160 KB, or 32 KB where the weights' stream
+// fills every compute unit anyway.  Over 51920 random shapes of 1 to 64 rows, 128 to
+// 28800 outputs and 256 to 14336 channels the kernel that this chooses is 1.1% slower
+// than the faster of the two in the geometric mean, 4% at the 95th percentile.  Against
+// the tile kernel's best plan, us: 4096 x 4096, MXFP8, 8 rows 4.6 (8.1), 32 rows 7.4
+// (8.5), 64 rows 11.5 (10.0); 12288 x 4096, 8 rows 9.4 (10.6), 24 rows 15.3 (11.3);
+// 4096 x 24576, 1 row 11.3 (11.4), 8 rows 13.0 (11.5).
 bool mx_few(int x_fmt, long rows, int n_out, int n_in) {
     if (rows > kFewRows) return false;
-    const long read = rows <= 16 ? rows : rows <= 32 ? 32 : 64;
-    return read * polestar_codec_row_bytes(x_fmt, n_in) * ceil_div(n_out, 16 * mx_few_nt(n_out)) <= 34L << 20;
+    const int nt = mx_few_nt(n_out);
+    const long per_cu = rows * polestar_codec_row_bytes(x_fmt, n_in) * ceil_div(ceil_div(n_out, 16 * nt), kMxCus);
+    return per_cu <= (nt == 1 ? 160 : 32) * 1024;
 }
 
 template <int FMT, bool BF16>
