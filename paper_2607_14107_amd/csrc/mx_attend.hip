@@ -26,6 +26,8 @@
 //
 // fp32 queries: q and p are taken as three bf16 terms each, so that the products
 // with the exact keys and values keep 24 bits.
+#include <algorithm>
+
 #include "host_common.hpp"
 #include "mx_dev.hpp"
 
@@ -380,9 +382,11 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_merge_kernel(MxAttArgs a
     if (a.lse && lane == 0) a.lse[(static_cast<size_t>(b) * a.heads + head) * a.n_rows + row] = (m + __log2f(l)) * kLn2;
 }
 
-// Waves per workgroup and key splits: eight waves where the workgroups are at most
-// the compute units (two waves on each SIMD, which the registers allow), and as
-// many splits as fill them, while a wave has two steps or more.
+// Waves per workgroup and key splits: eight waves where the workgroups are at most the
+// compute units and each wave has two steps (the registers allow two waves on each
+// SIMD), and then as many splits as fill the units in one round, while a wave keeps two
+// steps.  One token of two sequences over 32768 keys, 4 KV heads: 405 us without
+// splits, 13.4 with 32 and their join.
 struct MxAttPlan {
     int tiles, waves, splits;
     size_t part, total;                                  // bytes: O parts, with the sums
@@ -394,11 +398,7 @@ MxAttPlan mx_att_plan(int batch, int seq, int heads, int kv_heads, int hd, int n
     const long wgs = static_cast<long>(batch) * kv_heads * p.tiles;
     const int steps = ceil_div(seq, kMxKeys);
     p.waves = steps >= 16 && wgs <= 256 ? 8 : 4;
-    long splits = (p.waves == 8 ? 256 : 512) / wgs;
-    const long most = steps / (2 * p.waves);
-    if (splits > most) splits = most;
-    if (splits > kMxMaxSplits) splits = kMxMaxSplits;
-    p.splits = splits < 1 ? 1 : static_cast<int>(splits);
+    p.splits = p.waves == 8 ? static_cast<int>(std::min({256 / wgs, steps / 16L, static_cast<long>(kMxMaxSplits)})) : 1;
     if (p.splits > 1) {
         const size_t rows = static_cast<size_t>(batch) * kv_heads * p.splits * nq;
         p.part = align_up(rows * hd * sizeof(float), 256);

@@ -393,6 +393,9 @@ ATTEND = [  # b, seq, rows, heads, kv_heads, lens, packed, scale
     (1, 4100, 3, 8, 8, (4097,), False, 0.0),
     (5, 12, 2, 2, 1, (0, 0, -3, 12, 1), False, 0.0),
     (1, 9000, 1, 7, 1, (8999,), True, 0.0),
+    (8, 530, 2, 20, 20, (530, 0, 1, 511, 513, 32, 31, 600), False, 0.0),      # 160 workgroups: no split
+    (9, 513, 1, 30, 30, (513, 512, 17, 0, 480, 5, 513, 513, 100), True, 0.0),  # 270 workgroups
+    (1, 33000, 1, 4, 1, (32999,), False, 0.0),                                # the most splits
 ]
 
 
