@@ -457,6 +457,8 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
 // rows x 16 NT outputs per workgroup; its waves take chunks of 512 channels in turn
 // (256 bytes of a weight row, 16 of its scales), every load of a chunk issued before
 // its first product, and their sums are added in LDS: no split and no second launch.
+// One row of 4096 x 4096 takes 3.5 us in a graph (8.9 MB at 2.5 TB/s), of 4096 x 24576
+// 11.3 (53 MB at 4.7).
 //
 // RAW: the rows come as dtype and are quantized here, a lane the block that it holds
 // (32 channels: no exchange for the maximum), so that one launch does both; every
