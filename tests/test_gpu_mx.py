@@ -586,6 +586,40 @@ def test_layer_forward_in_a_graph(P):
         assert all(torch.equal(x, y) for x, y in zip(a.results(), want))
 
 
+def test_workspaces_that_are_missing_or_too_small(P):
+    """Split products and attention on a side stream, their scratch and outputs made by the call: the same bits."""
+    torch = _torch()
+    g = np.random.default_rng(4)
+    x = _dev(g.standard_normal((1, 80, 4096)).astype(np.float32)).bfloat16()
+    w = P.mx_quantize(P.MXFP4, _dev(g.standard_normal((512, 4096)).astype(np.float32)))
+    h = P.mx_quantize(P.MXFP8, x)
+    caches = [t.view(2, 1, 4096, -1) for _ in range(2)
+              for t in P.mx_quantize(P.MXFP4, _dev(g.standard_normal((8192, 128)).astype(np.float32)))]
+    q = _dev(g.standard_normal((2, 3, 5, 128)).astype(np.float32)).bfloat16()
+    sizes = [P.mx_linear_workspace_size(P.MXFP8, P.BF16, 80, 512, 4096),
+             P.mx_quantize_linear_workspace_size(P.MXFP8, P.BF16, 1, 80, 512, 4096),
+             P.mx_attend_workspace_size(P.BF16, 2, 4096, 5, 1, 128, 3)]
+    assert all(sizes)
+    y = lambda: torch.zeros((1, 80, 512), dtype=torch.bfloat16, device="cuda")  # noqa: E731
+
+    def run(ws, **kw):
+        return [P.mx_linear(P.MXFP8, *h, *w, y(), workspace=ws[0], **kw),
+                P.mx_quantize_linear(P.MXFP8, x, 0, 80, *w, y(), workspace=ws[1], **kw),
+                P.mx_attend(q, *caches, workspace=ws[2], **kw)]
+    want = run([torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes])
+    small = run([torch.empty(16, dtype=torch.uint8, device="cuda")] * 3)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        current = run([None] * 3)
+    side.synchronize()
+    for got in (small, current):
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    out = P.mx_attend(q, *caches, stream=side)              # a stream that is not the current one
+    side.synchronize()
+    assert torch.equal(out, want[2])
+
+
 def test_no_rows_is_no_work(P):
     torch = _torch()
     u8 = lambda *s: torch.empty(s, dtype=torch.uint8, device="cuda")  # noqa: E731
