@@ -278,11 +278,11 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     __builtin_amdgcn_s_waitcnt(mx_wait_vm((NS - 1) * ND));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    // K tile t, in slot U, whose round's scales are in buffer `buf`.  (The slots are
+    // K tile t, in slot U, whose scales are in buffer `buf`.  (The slots are
     // constants: with a slot that moves, each read's address is computed behind the
     // barrier, 8% slower.)
     auto slot_of = [&](int u) { return lds + u % NS * T::kSlot; };
-    auto scales_of = [&](int step, int buf) {            // of a step of this round, or the next round's first
+    auto scales_of = [&](int step, int buf) {            // of a step of the buffer's R, or the first of the next R
         return step < T::R ? Scales{buf, step} : Scales{buf ^ T::kScales, 0};
     };
     int buf = 0, t = 0;
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
         for (; t + kUnroll <= whole; t += kUnroll, buf ^= T::kScales)
             mx_unrolled([&](auto u) {
                 ktile(t + u, u);
-                if (u == 0) issue_scales(t + kUnroll, buf ^ T::kScales);   // landed by the last sync of this round
+                if (u == 0) issue_scales(t + kUnroll, buf ^ T::kScales);   // landed by the last sync before they are read
             }, std::make_integer_sequence<int, kUnroll>{});
         mx_unrolled([&](auto u) {
             if (t + u < whole) ktile(t + u, u);
