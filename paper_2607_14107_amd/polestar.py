@@ -201,6 +201,20 @@ def _stream(stream) -> int:
     return s.cuda_stream
 
 
+def _empty(shape, dtype: torch.dtype, device, stream, returned: bool = True) -> torch.Tensor:
+    """A new tensor for work on `stream` (None: the current one), of that stream's own memory: a block of the
+    current stream's may still be in use by work queued there, for which `stream` does not wait.  One that is
+    returned may be read on the current stream, so it is kept from reuse until that is done too."""
+    current = None if stream is None else torch.cuda.current_stream()
+    if stream is None or stream == current:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(current)
+    return t
+
+
 def _workspace(nbytes: int, device, ws: torch.Tensor | None) -> torch.Tensor | None:
     if nbytes == 0:
         return ws
@@ -631,12 +645,9 @@ def _mx_stream(dev: int, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
-def _mx_empty(shape, dtype, dev: int, stream) -> torch.Tensor:
-    """A new tensor for work on `stream`: kept from reuse until that is done where it is not the current stream."""
-    t = torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
-    if stream is not None and stream != torch.cuda.current_stream():
-        t.record_stream(stream)
-    return t
+def _mx_empty(shape, dtype, dev: int, stream, returned: bool = True) -> torch.Tensor:
+    """_empty on the device of this index."""
+    return _empty(shape, dtype, torch.device("cuda", dev), stream, returned)
 
 
 def _mx_call(name: str, args: tuple, size, ws: torch.Tensor | None, dev: int, stream) -> None:
@@ -649,7 +660,7 @@ def _mx_call(name: str, args: tuple, size, ws: torch.Tensor | None, dev: int, st
         status = f(*args, _mx_ptr(ws, ws.dtype), ws.numel() * ws.element_size(), st)
     if status == STATUS_WORKSPACE:
         nbytes = size()
-        ws = _mx_empty(nbytes, torch.uint8, dev, stream) if nbytes else None
+        ws = _mx_empty(nbytes, torch.uint8, dev, stream, returned=False) if nbytes else None
         status = f(*args, None if ws is None else ws.data_ptr(), nbytes, st)
     _check(name, status)
 

@@ -1,0 +1,82 @@
+"""Calls that make their own outputs and scratch on a stream that is not the current
+one, while work queued on the current stream still writes to memory that it has just
+given back: the results are those of the same calls on an idle GPU."""
+
+import pytest
+
+from tests._util import ensure_built
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def P():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    ensure_built()
+    from paper_2607_14107_amd import polestar
+    return polestar
+
+
+def _normal(*shape, seed=0, dtype=None):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed + sum(shape))
+    return torch.randn(shape, generator=g, device="cuda").to(dtype or torch.bfloat16)
+
+
+def _beside_work_in_progress(call, sizes):
+    """call(stream) -> tensors: its results on a side stream, issued while the current stream is about to fill
+    blocks of these sizes (bytes) that were freed already."""
+    import torch
+    want = call(None)
+    want = [t.clone() for t in want]
+    busy = _normal(4096, 4096)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    blocks = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+    for _ in range(40):                                  # some milliseconds
+        busy = (busy @ busy).clamp_(-1, 1)
+    for b in blocks:
+        b.fill_(0xFF)
+    del blocks, b
+    got = call(side)
+    torch.cuda.synchronize()
+    assert len(got) == len(want)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_microscaled_rows_and_their_scales(P):
+    x = _normal(3, 200, 4096)
+    n = x.numel()
+    _beside_work_in_progress(lambda s: P.mx_quantize(P.MXFP8, x, stream=s), [n, n // 32])
+
+
+def test_microscaled_product(P):
+    import torch
+    w = P.mx_quantize(P.MXFP4, _normal(512, 4096))
+    h = P.mx_quantize(P.MXFP8, _normal(80, 4096))
+    y = torch.zeros((80, 512), dtype=torch.bfloat16, device="cuda")
+    need = P.mx_linear_workspace_size(P.MXFP8, P.BF16, 80, 512, 4096)
+    assert need                                          # a split product: sums pass through the scratch
+    _beside_work_in_progress(lambda s: [P.mx_linear(P.MXFP8, *h, *w, y, stream=s)], [need])
+
+
+def test_microscaled_product_of_rows(P):
+    import torch
+    w = P.mx_quantize(P.MXFP4, _normal(512, 4096))
+    x = _normal(1, 80, 4096)
+    y = torch.zeros((1, 80, 512), dtype=torch.bfloat16, device="cuda")
+    need = P.mx_quantize_linear_workspace_size(P.MXFP8, P.BF16, 1, 80, 512, 4096)
+    assert need
+    _beside_work_in_progress(lambda s: [P.mx_quantize_linear(P.MXFP8, x, 0, 80, *w, y, stream=s)], [need])
+
+
+def test_microscaled_attention(P):
+    caches = [t.view(2, 1, 4096, -1) for i in range(2) for t in P.mx_quantize(P.MXFP4, _normal(8192, 128, seed=i))]
+    q = _normal(2, 3, 5, 128)
+    need = P.mx_attend_workspace_size(P.BF16, 2, 4096, 5, 1, 128, 3)
+    assert need
+    _beside_work_in_progress(lambda s: [P.mx_attend(q, *caches, stream=s)], [need, 2 * q.numel()])
