@@ -215,13 +215,13 @@ def _empty(shape, dtype: torch.dtype, device, stream, returned: bool = True) -> 
     return t
 
 
-def _workspace(nbytes: int, device, ws: torch.Tensor | None) -> torch.Tensor | None:
+def _workspace(nbytes: int, device, ws: torch.Tensor | None, stream=None) -> torch.Tensor | None:
     if nbytes == 0:
         return ws
     if ws is not None and ws.numel() * ws.element_size() >= nbytes:
         return ws
     # the library needs no initialised workspace
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _empty(nbytes, torch.uint8, device, stream, returned=False)
 
 
 # ---------------------------------------------------------------------------
@@ -235,7 +235,7 @@ def drift(h_cur: torch.Tensor, h_prev: torch.Tensor, out: torch.Tensor | None = 
     if h_prev.shape != h_cur.shape or h_prev.dtype != h_cur.dtype:
         raise ValueError("h_cur and h_prev differ in shape or dtype")
     if out is None:
-        out = torch.empty((b, s), dtype=torch.float32, device=h_cur.device)
+        out = _empty((b, s), torch.float32, h_cur.device, stream)
     _check("polestar_drift", lib().polestar_drift(_dtype_code(h_cur), b, s, d, _ptr(h_cur), _ptr(h_prev),
                                                  _ptr(out, torch.float32), _stream(stream)))
     return out
@@ -248,9 +248,9 @@ def select(drift_vals: torch.Tensor, k: int, block_start: int, block_len: int,
     b, s = drift_vals.shape
     dev = drift_vals.device
     if stale_idx is None:
-        stale_idx = torch.empty((b, max(k, 0)), dtype=torch.int32, device=dev)
+        stale_idx = _empty((b, max(k, 0)), torch.int32, dev, stream)
     if stale_count is None:
-        stale_count = torch.empty((b,), dtype=torch.int32, device=dev)
+        stale_count = _empty((b,), torch.int32, dev, stream)
     _check("polestar_select", lib().polestar_select(
         b, s, _ptr(drift_vals, torch.float32), _ptr(eligible, torch.uint8), block_start, block_len, k,
         _ptr(stale_idx, torch.int32) if k > 0 else None, _ptr(stale_count, torch.int32), _stream(stream)))
@@ -271,7 +271,7 @@ def refresh_kv(h_cur: torch.Tensor, stale_idx: torch.Tensor | None, stale_count:
     _, _, kvh, hd = k_cache.shape
     dt = _dtype_code(h_cur)
     k_max = 0 if stale_idx is None else stale_idx.shape[1]
-    ws = _workspace(refresh_kv_workspace_size(dt, b, d, kvh, hd, k_max, block_len), h_cur.device, workspace)
+    ws = _workspace(refresh_kv_workspace_size(dt, b, d, kvh, hd, k_max, block_len), h_cur.device, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_refresh_kv", lib().polestar_refresh_kv(
         dt, b, s, d, kvh, hd, _ptr(h_cur),
@@ -317,7 +317,7 @@ def project_qkv(h_cur: torch.Tensor, row_start: int, n_rows: int, w_q: torch.Ten
     if tuple(q.shape) != (b, n_rows, heads, hd) or tuple(w_q.shape) != (heads * hd, d):
         raise ValueError("project_qkv: shapes do not match")
     dt = _dtype_code(h_cur)
-    ws = _workspace(project_qkv_workspace_size(dt, b, d, heads, kvh, hd, n_rows), h_cur.device, workspace)
+    ws = _workspace(project_qkv_workspace_size(dt, b, d, heads, kvh, hd, n_rows), h_cur.device, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_project_qkv", lib().polestar_project_qkv(
         dt, b, s, d, heads, kvh, hd, _ptr(h_cur), row_start, n_rows, _ptr(w_q, h_cur.dtype), _ptr(w_k, h_cur.dtype),
@@ -338,8 +338,8 @@ def project_q(h_cur: torch.Tensor, w_q: torch.Tensor, block_start: int, block_le
     hd = w_q.shape[0] // n_heads
     dt = _dtype_code(h_cur)
     if out is None:
-        out = torch.empty((b, block_len, n_heads, hd), dtype=h_cur.dtype, device=h_cur.device)
-    ws = _workspace(project_q_workspace_size(dt, b, d, n_heads, hd, block_len), h_cur.device, workspace)
+        out = _empty((b, block_len, n_heads, hd), h_cur.dtype, h_cur.device, stream)
+    ws = _workspace(project_q_workspace_size(dt, b, d, n_heads, hd, block_len), h_cur.device, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_project_q", lib().polestar_project_q(
         dt, b, s, d, n_heads, hd, block_start, block_len, _ptr(h_cur), _ptr(w_q, h_cur.dtype),
@@ -366,10 +366,10 @@ def attend(h_cur: torch.Tensor | None, w_q: torch.Tensor | None, k_cache: torch.
     dev = k_cache.device
     d = h_cur.shape[2] if h_cur is not None else n_heads * hd
     if q_buf is None:
-        q_buf = torch.empty((b, block_len, n_heads, hd), dtype=k_cache.dtype, device=dev)
+        q_buf = _empty((b, block_len, n_heads, hd), k_cache.dtype, dev, stream)
     if out is None:
-        out = torch.empty((b, block_len, n_heads, hd), dtype=k_cache.dtype, device=dev)
-    ws = _workspace(attend_workspace_size(dt, b, s, d, n_heads, kvh, hd, block_len), dev, workspace)
+        out = _empty((b, block_len, n_heads, hd), k_cache.dtype, dev, stream)
+    ws = _workspace(attend_workspace_size(dt, b, s, d, n_heads, kvh, hd, block_len), dev, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_attend", lib().polestar_attend(
         dt, b, s, d, n_heads, kvh, hd, block_start, block_len,
@@ -396,12 +396,12 @@ def commit(logits: torch.Tensor, masked: torch.Tensor, drift_vals: torch.Tensor 
     seq = drift_vals.shape[1] if drift_vals is not None else 0
     h = hist.shape[1] if hist is not None else 0
     if token is None:
-        token = torch.empty((b, nq), dtype=torch.int32, device=dev)
+        token = _empty((b, nq), torch.int32, dev, stream)
     if conf is None:
-        conf = torch.empty((b, nq), dtype=torch.float32, device=dev)
+        conf = _empty((b, nq), torch.float32, dev, stream)
     if commit_out is None:
-        commit_out = torch.empty((b, nq), dtype=torch.uint8, device=dev)
-    ws = _workspace(commit_workspace_size(dt, b, nq, vocab), dev, workspace)
+        commit_out = _empty((b, nq), torch.uint8, dev, stream)
+    ws = _workspace(commit_workspace_size(dt, b, nq, vocab), dev, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_commit", lib().polestar_commit(
         dt, b, nq, vocab, _ptr(logits), _ptr(masked, torch.uint8), _ptr(drift_vals, torch.float32), seq,
@@ -420,12 +420,12 @@ def suffix_commit(logits: torch.Tensor, masked: torch.Tensor, eligible: torch.Te
     dt = _dtype_code(logits)
     dev = logits.device
     if token is None:
-        token = torch.empty((b, n), dtype=torch.int32, device=dev)
+        token = _empty((b, n), torch.int32, dev, stream)
     if conf is None:
-        conf = torch.empty((b, n), dtype=torch.float32, device=dev)
+        conf = _empty((b, n), torch.float32, dev, stream)
     if commit_out is None:
-        commit_out = torch.empty((b, n), dtype=torch.uint8, device=dev)
-    ws = _workspace(commit_workspace_size(dt, b, n, vocab), dev, workspace)
+        commit_out = _empty((b, n), torch.uint8, dev, stream)
+    ws = _workspace(commit_workspace_size(dt, b, n, vocab), dev, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_suffix_commit", lib().polestar_suffix_commit(
         dt, b, n, vocab, _ptr(logits), _ptr(masked, torch.uint8), _ptr(eligible, torch.uint8), mask_token_id,
@@ -475,7 +475,7 @@ def linear(x: torch.Tensor, row_start: int, n_rows: int, w: torch.Tensor, y: tor
     if tuple(y.shape) != (b, n_rows, n_out) or w.shape[1] != n_in:
         raise ValueError("linear: shapes do not match")
     dt = _dtype_code(x)
-    ws = _workspace(linear_workspace_size(dt, b, n_rows, n_out, n_in), x.device, workspace)
+    ws = _workspace(linear_workspace_size(dt, b, n_rows, n_out, n_in), x.device, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_linear", lib().polestar_linear(
         dt, b, seq, n_in, n_out, row_start, n_rows, _ptr(x), _ptr(w, x.dtype), _ptr(y, x.dtype), _ptr(ws), nbytes,
@@ -524,7 +524,7 @@ def linear_swiglu(x: torch.Tensor, row_start: int, n_rows: int, w_gate_up: torch
             or tuple(w_gate_up.shape) != (2 * f, n_in)):
         raise ValueError("linear_swiglu: shapes do not match")
     dt = _dtype_code(x)
-    ws = _workspace(linear_workspace_size(dt, b, n_rows, 2 * f, n_in), x.device, workspace)
+    ws = _workspace(linear_workspace_size(dt, b, n_rows, 2 * f, n_in), x.device, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_linear_swiglu", lib().polestar_linear_swiglu(
         dt, b, seq, n_in, f, row_start, n_rows, _ptr(x), _ptr(w_gate_up, x.dtype), _ptr(gate_up, x.dtype),
@@ -579,7 +579,7 @@ def cluster_means(x: torch.Tensor, win_idx: torch.Tensor, labels: torch.Tensor, 
     """Per cluster the mean of its window members' rows of x [b][seq][d] (float32) -> [b][K][d]."""
     b, seq, d = x.shape
     if means is None:
-        means = torch.empty((b, n_clusters, d), dtype=torch.float32, device=x.device)
+        means = _empty((b, n_clusters, d), torch.float32, x.device, stream)
     _check("polestar_cluster_means", lib().polestar_cluster_means(
         b, seq, d, _ptr(x, torch.float32), _ptr(win_idx, torch.int32), win_idx.shape[1], _ptr(labels, torch.int32),
         n_clusters, _ptr(means, torch.float32), _stream(stream)))
@@ -871,10 +871,10 @@ def cluster(h: torch.Tensor, win_idx: torch.Tensor, n_clusters: int, iters: int 
     b, seq, d = h.shape
     dev = h.device
     n_win = win_idx.shape[1]
-    labels = torch.empty((b, seq), dtype=torch.int32, device=dev)
-    sums = torch.empty((b, n_clusters, d), dtype=torch.float32, device=dev)
-    counts = torch.empty((b, n_clusters), dtype=torch.int32, device=dev)
-    cents = torch.empty((b, n_clusters, d), dtype=torch.float32, device=dev)
+    labels = _empty((b, seq), torch.int32, dev, stream)
+    sums = _empty((b, n_clusters, d), torch.float32, dev, stream)
+    counts = _empty((b, n_clusters), torch.int32, dev, stream)
+    cents = _empty((b, n_clusters, d), torch.float32, dev, stream)
     _check("polestar_cluster", lib().polestar_cluster(
         _dtype_code(h), b, seq, d, _ptr(h), _ptr(win_idx, torch.int32), n_win, n_clusters, iters,
         _ptr(labels), _ptr(sums), _ptr(counts), _ptr(cents), _stream(stream)))
@@ -896,8 +896,8 @@ def proxy_drift(sums: torch.Tensor, counts: torch.Tensor, w_q: torch.Tensor, k_c
     _, seq, kvh, hd = k_cache.shape
     dt = _dtype_code(k_cache)
     if drift_out is None:
-        drift_out = torch.empty((b, K), dtype=torch.float32, device=sums.device)
-    ws = _workspace(proxy_drift_workspace_size(dt, b, seq, d, n_heads, hd, K), sums.device, workspace)
+        drift_out = _empty((b, K), torch.float32, sums.device, stream)
+    ws = _workspace(proxy_drift_workspace_size(dt, b, seq, d, n_heads, hd, K), sums.device, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_proxy_drift", lib().polestar_proxy_drift(
         dt, b, seq, d, n_heads, kvh, hd, K, _ptr(sums, torch.float32), _ptr(counts, torch.int32),
@@ -920,8 +920,8 @@ def attention_drift(q: torch.Tensor, k_cache: torch.Tensor, scores: torch.Tensor
     b, R, H, hd = q.shape
     _, seq, kvh, _ = k_cache.shape
     if drift_out is None:
-        drift_out = torch.empty((b, R), dtype=torch.float32, device=q.device)
-    ws = _workspace(attention_drift_workspace_size(b, seq, R, H), q.device, workspace)
+        drift_out = _empty((b, R), torch.float32, q.device, stream)
+    ws = _workspace(attention_drift_workspace_size(b, seq, R, H), q.device, workspace, stream)
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     _check("polestar_attention_drift", lib().polestar_attention_drift(
         _dtype_code(q), b, seq, R, H, kvh, hd, _ptr(q), _ptr(k_cache, q.dtype), float(scale),
@@ -938,9 +938,9 @@ def cluster_select(labels: torch.Tensor, drift_vals: torch.Tensor, k_top: int, k
     K = drift_vals.shape[1]
     dev = labels.device
     if stale_idx is None:
-        stale_idx = torch.empty((b, k_max), dtype=torch.int32, device=dev)
+        stale_idx = _empty((b, k_max), torch.int32, dev, stream)
     if stale_count is None:
-        stale_count = torch.empty((b,), dtype=torch.int32, device=dev)
+        stale_count = _empty((b,), torch.int32, dev, stream)
     _check("polestar_cluster_select", lib().polestar_cluster_select(
         b, seq, _ptr(labels, torch.int32), K, _ptr(drift_vals, torch.float32), k_top,
         _ptr(stale_idx, torch.int32) if k_max > 0 else None, k_max, _ptr(stale_count, torch.int32),

@@ -80,3 +80,38 @@ def test_microscaled_attention(P):
     need = P.mx_attend_workspace_size(P.BF16, 2, 4096, 5, 1, 128, 3)
     assert need
     _beside_work_in_progress(lambda s: [P.mx_attend(q, *caches, stream=s)], [need, 2 * q.numel()])
+
+
+def test_attention_over_a_cache(P):
+    k, v, q = _normal(1, 2048, 2, 128), _normal(1, 2048, 2, 128, seed=1), _normal(1, 32, 2, 128)
+    need = P.attend_workspace_size(P.BF16, 1, 2048, 256, 2, 2, 128, 32)
+    assert need
+    _beside_work_in_progress(lambda s: [P.attend(None, None, k, v, 64, 32, 2, q_buf=q, stream=s)[0]],
+                             [need, 2 * q.numel()])
+
+
+def test_product_of_dense_rows(P):
+    import torch
+    x, w = _normal(1, 128, 4096), _normal(1024, 4096)
+    y = torch.zeros((1, 96, 1024), dtype=torch.bfloat16, device="cuda")
+    need = P.linear_workspace_size(P.BF16, 1, 96, 1024, 4096)
+    assert need
+    _beside_work_in_progress(lambda s: [P.linear(x, 8, 96, w, y, stream=s)], [need])
+
+
+def test_drift_and_select(P):
+    a, b = _normal(2, 3000, 1024), _normal(2, 3000, 1024, seed=1)
+
+    def both(s):
+        d = P.drift(a, b, stream=s)
+        return [d, *P.select(d, 40, 64, 32, stream=s)]
+    _beside_work_in_progress(both, [4 * 2 * 3000, 4 * 2 * 40, 8])
+
+
+def test_commit(P):
+    import torch
+    logits = _normal(1, 32, 126464)
+    masked = torch.ones((1, 32), dtype=torch.uint8, device="cuda")
+    need = P.commit_workspace_size(P.BF16, 1, 32, 126464)
+    assert need
+    _beside_work_in_progress(lambda s: P.suffix_commit(logits, masked, masked, stream=s), [need, 128, 128, 32])
