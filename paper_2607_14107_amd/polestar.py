@@ -642,7 +642,11 @@ def _mx_ptr(t: torch.Tensor | None, dtype: torch.dtype) -> int | None:
 
 
 def _mx_stream(dev: int, stream) -> int:
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError(f"tensors are on cuda:{dev}, the stream is of cuda:{stream.device_index}")
+    return stream.cuda_stream
 
 
 def _mx_empty(shape, dtype, dev: int, stream, returned: bool = True) -> torch.Tensor:

@@ -129,3 +129,9 @@ def test_calls_allocate_on_the_stream_they_run_on(made, monkeypatch, name):
         assert [a for _, a in launched] == [s.cuda_stream]
         assert [a for a, _ in made] == [s] * (returned + (name in SCRATCH))
         assert [a for _, a in recorded] == ([main] * returned if stream else [])
+
+
+def test_microscaled_calls_refuse_a_stream_of_another_device():
+    assert ps._mx_stream(0, _Stream(7)) == 7
+    with pytest.raises(ValueError, match="stream"):
+        ps._mx_stream(0, _Stream(7, device_index=1))
