@@ -89,7 +89,8 @@ constexpr int kMxCus = 256;
 // lane's offset is one register, the K tile's a scalar; the lanes land one after
 // another from lds on.  Written out, because the compiler waits for every transfer
 // that it knows of before it reads LDS; the waits are the kernel's own (mx_wait_vm
-// before the barrier that hands a slot over).
+// before the barrier that hands a slot over).  m0 is a register that the compiler
+// reserves, hence its warning, but values of its own in m0 have to end here.
 typedef uint32_t MxBuffer __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ MxBuffer mx_buffer(const void* base, uint32_t bytes) {
@@ -99,10 +100,13 @@ __device__ __forceinline__ MxBuffer mx_buffer(const void* base, uint32_t bytes) 
 __device__ __forceinline__ uint32_t lds_offset(const char* p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
 }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void mx_dma16(MxBuffer b, uint32_t lane_off, uint32_t off, const char* lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :: "s"(uniform(lds_offset(lds))), "v"(lane_off), "s"(b), "s"(uniform(off)) : "memory");
+                 :: "s"(uniform(lds_offset(lds))), "v"(lane_off), "s"(b), "s"(uniform(off)) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // s_waitcnt immediates: at most n vector-memory operations outstanding / LDS reads done
 constexpr int mx_wait_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
 constexpr int kMxWaitLgkm0 = 15 | (3 << 14) | (7 << 4);
