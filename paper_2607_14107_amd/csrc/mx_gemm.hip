@@ -471,6 +471,7 @@ __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
 
 constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave;
 constexpr int kFewRows = 64;                             // most rows of these kernels
+constexpr int kFewSteps = 4;                             // steps of a chunk, of 128 channels
 
 struct MxFewArgs : MxGemmArgs {
     const char* raw;                                     // [batch][seq][n_in] dtype
@@ -541,8 +542,8 @@ __global__ __launch_bounds__(kFewThreads) void mx_few_kernel(MxFewArgs g) {
     constexpr bool DEC = FMT == POLESTAR_MXFP8 && !BF16;
     constexpr bool kSwap = RAW && FMT == POLESTAR_MXFP8 && !DEC;   // blocks in the order 0, 2, 1, 3
     constexpr int ES = BF16 ? 2 : 4;
-    constexpr int S = 4;                                 // steps of a chunk
-    static_assert(!RAW || MT == 1, "rows quantized here: one row tile");
+    constexpr int S = kFewSteps;
+    static_assert(!RAW || (MT == 1 && NT == 1), "rows quantized here: one tile");
     __shared__ floatx4 red[kFewWaves][MT * NT][kWave];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, grp = lane >> 4;
@@ -748,7 +749,7 @@ void mx_launch_few(const MxFewArgs& g, int nt, hipStream_t stream) {
     if (kDec && g.rows > 32) nt = 1;
     const dim3 grid(ceil_div(g.n_out, 16 * nt)), block(kFewThreads);
 #define PS_FEW(RAW, MT, NT) hipLaunchKernelGGL((mx_few_kernel<FMT, BF16, RAW, MT, NT>), grid, block, 0, stream, g)
-    if (g.raw) { if (nt == 1) PS_FEW(true, 1, 1); else PS_FEW(true, 1, 2); }
+    if (g.raw) PS_FEW(true, 1, 1);                       // (mx_few_raw: as many workgroups as compute units at most)
     else if (g.rows <= 16) { if (nt == 1) PS_FEW(false, 1, 1); else PS_FEW(false, 1, 2); }
     else if (g.rows <= 32) { if (nt == 1) PS_FEW(false, 2, 1); else PS_FEW(false, 2, 2); }
     else if constexpr (!kDec) { if (nt == 1) PS_FEW(false, 4, 1); else PS_FEW(false, 4, 2); }
@@ -839,12 +840,17 @@ bool mx_shape_ok(long rows, int n_out, int n_in) {
     return n_in % 128 == 0 && n_out % 16 == 0 && rows <= (1L << 24) && n_out <= (1 << 22) && n_in <= (1 << 22);
 }
 
-// Rows that the product's kernel quantizes itself: up to 16, and few enough
-// workgroups that repeat it.  Against two launches, us: 4096 x 4096, bf16, 1 row 5.9
-// (5.9) and one launch less for the host, 16 rows 7.2 (7.0), fp32 4 rows 6.9 (6.8),
-// 16 rows 11.0 (7.4); 1024 x 256 3.7 (6.0); 12288 x 4096, bf16, 1 row 12.8 (10.3).
+// Rows that the product's kernel quantizes itself: up to 16 (fp32 4), where a wave has
+// one chunk of the rows and a compute unit one workgroup.  One launch less is 2.7 us
+// less on the host (6.9 instead of 9.6 us a call, queued one after another).  In a
+// graph, against two launches, us: 2048 channels and less gain up to a fifth (1024 x
+// 1024, 1 to 16 rows 3.2 to 4.1, 3.7 to 4.4), 4096 x 4096 costs up to a tenth more (bf16
+// MXFP8, 1 row 6.6, 6.3; 16 rows 8.2, 7.7; fp32, 4 rows 7.8, 6.9; 16 rows 11.9, 8.1).
+// Past the limits every workgroup quantizes chunk after chunk of the same rows: 4224 x
+// 256 6.7 (4.9), 8192 x 2048 10.1 (7.5), 65536 x 256 53 (29), and with two output tiles
+// 512 x 8192 6.5 (4.5), 4096 x 12288 14.1 (11.7).
 bool mx_few_raw(bool bf16, long rows, int n_out, int n_in) {
-    return rows <= (bf16 ? 16 : 4) && static_cast<long>(ceil_div(n_out, 16 * mx_few_nt(n_out))) * n_in <= 1L << 20;
+    return rows <= (bf16 ? 16 : 4) && n_in <= 128 * kFewSteps * kFewWaves && ceil_div(n_out, 16) <= kMxCus;
 }
 
 // Workspace of the quantized rows: codes, then scales.

@@ -64,8 +64,8 @@ def test_linear_of_few_long_rows(P, fmt, dtype, rows, n_in, n_out):
     _linear(P, np.random.default_rng(rows + n_in), fmt, dtype, rows, n_in, n_out, 2)
 
 
-# The rows quantized by the product's own kernel (up to 16 rows of bf16, 4 of fp32, n_in times the workgroups of
-# 16 outputs up to 2^20) and, at the same lengths, by a launch before it.
+# The rows quantized by the product's own kernel (up to 16 rows of bf16, 4 of fp32, 4096 channels, 4096 outputs)
+# and by a launch before it.
 ROWS = [(1, 9, 8, 1, 4096, 256), (1, 1, 0, 1, 128, 16), (1, 3, 1, 1, 4224, 144), (2, 4, 2, 2, 8192, 80),
         (1, 20, 4, 16, 8576, 272), (4, 5, 1, 4, 4480, 64), (1, 7, 3, 4, 12288, 528), (1, 2, 1, 1, 65536, 256),
         (1, 64, 3, 1, 4096, 4096), (1, 3, 0, 3, 4096, 8208)]
@@ -99,7 +99,7 @@ def test_quantize_linear_values(P, fmt, dtype, b, seq, start, rows, n_in, n_out)
 
 @DTYPES
 @BOTH
-@pytest.mark.parametrize("rows,n_in", [(1, 512), (3, 1152), (16, 640), (1, 4224)])
+@pytest.mark.parametrize("rows,n_in", [(1, 512), (3, 1152), (16, 640), (1, 4224), (4, 4096)])
 def test_quantize_linear_reads_the_oracles_codes(P, fmt, dtype, rows, n_in):
     """Weights with a single 1 per output: the outputs are the rows' decoded channels, bit for bit (ties, values that
     saturate, zero blocks and blocks 2^60 apart among them)."""
