@@ -16,6 +16,7 @@ namespace ps {
 
 constexpr int kMxBlock = 32;                     // channels per scale
 
+inline bool mx_fmt_ok(int fmt) { return fmt == POLESTAR_MXFP4 || fmt == POLESTAR_MXFP8; }
 inline bool aligned_to(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 typedef int intx8 __attribute__((ext_vector_type(8)));

@@ -794,8 +794,6 @@ void mx_launch(const MxPlan& p, const MxGemmArgs& g, hipStream_t stream) {
     }
 }
 
-bool mx_fmt_ok(int fmt) { return fmt == POLESTAR_MXFP4 || fmt == POLESTAR_MXFP8; }
-
 size_t mx_linear_ws(int x_fmt, polestar_dtype dtype, long rows, int n_out, int n_in) {
     return mx_few(x_fmt, rows, n_out, n_in) ? 0 : mx_plan(x_fmt, dtype == POLESTAR_BF16, rows, n_out, n_in).ws_bytes;
 }

@@ -208,8 +208,6 @@ __global__ __launch_bounds__(kMxStoreThreads) void mx_store_kv_kernel(StoreArgs 
     }
 }
 
-bool mx_fmt_ok(int fmt) { return fmt == POLESTAR_MXFP4 || fmt == POLESTAR_MXFP8; }
-
 // Workgroups for n8 groups of eight channels; 0: more than a grid holds.
 unsigned groups_grid(long n8) {
     const long g = (n8 + kMxThreads - 1) / kMxThreads;   // a launch has less than 2^32 threads
