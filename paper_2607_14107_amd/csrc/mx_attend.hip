@@ -407,6 +407,13 @@ MxAttPlan mx_att_plan(int batch, int seq, int heads, int kv_heads, int hd, int n
     return p;
 }
 
+// Sizes that the kernels' indices, and the plan's numbers, hold (all positive).
+bool mx_att_shape_ok(int batch, int seq, int heads, int kv_heads, int hd, int n_rows) {
+    const long nq = static_cast<long>(heads / kv_heads) * n_rows;
+    return (hd == 64 || hd == 128) && batch <= 65535 && kv_heads <= 65535 && seq <= kMxMaxSeq &&
+           nq <= (0x7fffffL << 5) && (nq + kMxQ) / kMxQ * kv_heads <= 0x7fffff;
+}
+
 template <bool BF16, int HD>
 void mx_att_launch(const MxAttPlan& p, const MxAttArgs& a, int batch, hipStream_t stream) {
     const dim3 grid(p.tiles * a.kv_heads, p.splits, batch);
@@ -428,7 +435,7 @@ extern "C" size_t polestar_mx_attend_workspace_size(polestar_dtype dtype, int ba
                                                     int n_kv_heads, int head_dim, int n_rows) {
     using namespace ps;
     if (!dtype_ok(dtype) || batch <= 0 || seq <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_rows <= 0 ||
-        n_heads % n_kv_heads != 0 || (head_dim != 64 && head_dim != 128))
+        n_heads % n_kv_heads != 0 || !mx_att_shape_ok(batch, seq, n_heads, n_kv_heads, head_dim, n_rows))
         return 0;
     return mx_att_plan(batch, seq, n_heads, n_kv_heads, head_dim, n_rows).total;
 }
@@ -444,11 +451,9 @@ extern "C" polestar_status polestar_mx_attend(polestar_dtype dtype, int batch, i
         n_heads % n_kv_heads != 0 || q_stride < static_cast<long>(n_heads) * head_dim || !q || !k_codes || !k_scales ||
         !v_codes || !v_scales || !out)
         return POLESTAR_ERR_INVALID_ARGUMENT;
-    const long nq = static_cast<long>(n_heads / n_kv_heads) * n_rows;
-    if ((head_dim != 64 && head_dim != 128) || !row_ok(dtype, q_stride) || !aligned16(q) || !aligned16(k_codes) ||
-        !aligned16(v_codes) || !aligned_to(k_scales, head_dim / kMxBlock) || !aligned_to(v_scales, head_dim / kMxBlock) ||
-        !aligned16(out) || !aligned16(workspace) || batch > 65535 || n_kv_heads > 65535 ||
-        (nq + kMxQ) / kMxQ * n_kv_heads > 0x7fffff || seq > kMxMaxSeq)
+    if (!mx_att_shape_ok(batch, seq, n_heads, n_kv_heads, head_dim, n_rows) || !row_ok(dtype, q_stride) ||
+        !aligned16(q) || !aligned16(k_codes) || !aligned16(v_codes) || !aligned_to(k_scales, head_dim / kMxBlock) ||
+        !aligned_to(v_scales, head_dim / kMxBlock) || !aligned16(out) || !aligned16(workspace))
         return POLESTAR_ERR_UNSUPPORTED;
     const MxAttPlan p = mx_att_plan(batch, seq, n_heads, n_kv_heads, head_dim, n_rows);
     if (workspace_bytes < p.total || (p.total > 0 && !workspace)) return POLESTAR_ERR_WORKSPACE;

@@ -1,5 +1,4 @@
-"""CPU tests of which rows the microscaled product quantizes itself, seen in the workspace that
-it asks for (none: nothing is quantized in a launch before it)."""
+"""CPU tests of the microscaled calls' plans, seen in the workspaces that they ask for."""
 
 import pytest
 
@@ -16,6 +15,7 @@ def _need(dtype, rows, n_in, n_out, fmt=ps.MXFP8):
     return ps.mx_quantize_linear_workspace_size(fmt, dtype, 1, rows, n_out, n_in)
 
 
+# Rows that the product quantizes itself need no workspace.
 @pytest.mark.parametrize("fmt", [ps.MXFP4, ps.MXFP8])
 @pytest.mark.parametrize("dtype,most", [(ps.BF16, 16), (ps.FP32, 4)])
 def test_few_rows_of_one_chunk_per_wave_on_one_round_of_workgroups(fmt, dtype, most):
@@ -33,3 +33,19 @@ def test_long_rows_and_many_outputs_are_quantized_before(fmt, dtype, n_in, n_out
     on more than one workgroup per compute unit, 512 x 8192 two fifths longer.)"""
     for rows in (1, 2, 4):
         assert _need(dtype, rows, n_in, n_out, fmt) > 0
+
+
+BIG = 2 ** 31 - 1
+# batch seq heads kv_heads head_dim rows: more than a launch holds, in each number and in products that pass 32 or 64 bits
+REFUSED = [(1, 4096, 2 ** 18, 1, 128, 2 ** 19), (1, 4096, BIG, 1, 128, BIG), (65536, 64, 4, 4, 128, 1),
+           (1, 64, 65536, 65536, 128, 1), (1, 2 ** 24 + 1, 4, 4, 128, 1), (65535, 64, 65535, 65535, 128, BIG),
+           (BIG, BIG, BIG, BIG, 64, BIG), (1, 64, 1, 1, 64, 2 ** 28)]
+
+
+@pytest.mark.parametrize("b,seq,heads,kvh,hd,rows", REFUSED)
+def test_attention_sizes_of_refused_shapes(b, seq, heads, kvh, hd, rows):
+    """A size query answers 0 for what the call refuses, however large the numbers."""
+    assert ps.mx_attend_workspace_size(ps.BF16, b, seq, heads, kvh, hd, rows) == 0
+    fake = 0x10000                                       # 16-byte aligned, never dereferenced
+    assert ps.lib().polestar_mx_attend(ps.BF16, b, seq, heads, kvh, hd, rows, fake, heads * hd, fake, fake, fake, fake,
+                                       None, 0.0, fake, None, None, 0, None) == 2
