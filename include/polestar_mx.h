@@ -123,7 +123,7 @@ polestar_status polestar_residual_rmsnorm_mx(int fmt, polestar_dtype dtype, long
  *         [0, n_rows] (NULL with idx: n_rows)
  * Requires 0 <= n_rows, row_start + n_rows <= seq without idx, row_stride >=
  * n_kv_heads * head_dim.  UNSUPPORTED unless head_dim is 64 or 128, n_rows <
- * 2^23, batch < 2^16, a stride is a whole number of 16-byte chunks, and k, v and
+ * 2^23, batch and n_kv_heads < 2^16, a stride is whole 16-byte chunks, and k, v and
  * the codes are 16-byte, the scales 4-byte aligned (head_dim 64: 2-byte).
  */
 polestar_status polestar_mx_store_kv(polestar_dtype dtype, int batch, int seq, int n_kv_heads, int head_dim,

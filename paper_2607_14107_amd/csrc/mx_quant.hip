@@ -301,7 +301,7 @@ extern "C" polestar_status polestar_mx_store_kv(polestar_dtype dtype, int batch,
         return POLESTAR_ERR_INVALID_ARGUMENT;
     if ((head_dim != 64 && head_dim != 128) || !row_ok(dtype, row_stride) || !aligned16(k) || !aligned16(v) ||
         !aligned16(k_codes) || !aligned16(v_codes) || !aligned_to(k_scales, head_dim / kMxBlock) ||
-        !aligned_to(v_scales, head_dim / kMxBlock) || batch > 65535 || n_rows > 0x7fffff)
+        !aligned_to(v_scales, head_dim / kMxBlock) || batch > 65535 || n_kv_heads > 65535 || n_rows > 0x7fffff)
         return POLESTAR_ERR_UNSUPPORTED;
     if (n_rows == 0) return POLESTAR_OK;
     const StoreArgs a{static_cast<const char*>(k), static_cast<const char*>(v), row_stride, idx, count, row_start,

@@ -49,3 +49,11 @@ def test_attention_sizes_of_refused_shapes(b, seq, heads, kvh, hd, rows):
     fake = 0x10000                                       # 16-byte aligned, never dereferenced
     assert ps.lib().polestar_mx_attend(ps.BF16, b, seq, heads, kvh, hd, rows, fake, heads * hd, fake, fake, fake, fake,
                                        None, 0.0, fake, None, None, 0, None) == 2
+
+
+@pytest.mark.parametrize("kvh", [65536, 2 ** 25, 2 ** 31 - 1])
+def test_store_refuses_more_heads_than_the_attention_takes(kvh):
+    """2^26 heads of 128 are 2^31 groups of channels in a row's keys and values together."""
+    fake = 0x10000
+    assert ps.lib().polestar_mx_store_kv(ps.BF16, 1, 4, kvh, 128, 1, fake, fake, kvh * 128, None, None, 0, fake, fake,
+                                         fake, fake, None) == 2
