@@ -789,7 +789,7 @@ def residual_rmsnorm_mx(fmt: int, x: torch.Tensor, y: torch.Tensor | None, x_out
         raise ValueError("residual_rmsnorm_mx: shapes do not match")
     dev = _mx_device(x, y, x_out, codes, scales, gain)
     _check("polestar_residual_rmsnorm_mx", lib().polestar_residual_rmsnorm_mx(
-        fmt, BF16 if y is None else _dtype_code(y), values // d, d, _mx_ptr(x, torch.float32),
+        fmt, BF16 if y is None else _dtype_code(y), values // d if d else 0, d, _mx_ptr(x, torch.float32),
         None if y is None else _mx_ptr(y, y.dtype), _mx_ptr(gain, torch.float32), float(eps),
         _mx_ptr(x_out, torch.float32), _mx_ptr(codes, torch.uint8), _mx_ptr(scales, torch.uint8),
         _mx_stream(dev, stream)))

@@ -1,6 +1,6 @@
 """GPU parity of the microscaled products where few rows meet long ones, where scales lie
-far apart, and of the codes that the self-quantizing kernel makes (oracle: oracle/mx_ref.py;
-bounds: tests/test_gpu_mx.py)."""
+far apart, and of the codes that the self-quantizing kernel makes; rows without channels
+(oracle: oracle/mx_ref.py; bounds: tests/test_gpu_mx.py)."""
 
 import numpy as np
 import pytest
@@ -134,3 +134,16 @@ def test_quantize_linear_reads_the_oracles_codes(P, fmt, dtype, rows, n_in):
                                              (1000, 1152, 2064)])
 def test_linear_of_scales_far_apart(P, fmt, dtype, rows, n_in, n_out, spread):
     _linear(P, np.random.default_rng(rows + spread), fmt, dtype, rows, n_in, n_out, spread)
+
+
+def test_rows_without_channels_are_refused(P):
+    import torch
+    u8 = lambda *s: torch.empty(s, dtype=torch.uint8, device="cuda")  # noqa: E731
+    x = torch.empty((4, 0), device="cuda")
+    for call in (lambda: P.residual_rmsnorm_mx(P.MXFP8, x, None, None, u8(4, 0), u8(4, 0)),
+                 lambda: P.mx_dequantize(P.MXFP4, u8(4, 0), u8(4, 0), x),
+                 lambda: P.mx_quantize(P.MXFP4, x),
+                 lambda: P.mx_linear(P.MXFP8, u8(0, 0), u8(0, 0), u8(16, 0), u8(16, 0), torch.empty((0, 16), device="cuda"))):
+        with pytest.raises(P.PolestarError) as e:
+            call()
+        assert e.value.status == 1
