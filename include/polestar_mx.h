@@ -60,7 +60,9 @@ polestar_status polestar_mx_dequantize(int fmt, polestar_dtype dtype, long rows,
  * The matrix instruction on MXFP8 rows adds eight neighbouring products at a
  * time with about 14 bits below the largest of them; that error is far below
  * bf16's, and fp32 outputs of MXFP8 rows are computed on bf16 matrix instructions
- * from the decoded values instead, with exact products.
+ * from the decoded values instead, with exact products (but for channels of blocks
+ * with scale bytes 0 to 2, which are rounded to multiples of 2^-133).  Results of a
+ * magnitude below 2^-126 may be 0.
  * A NaN block makes NaN of every output it takes part in.
  * UNSUPPORTED unless n_in % 128 == 0, n_out % 16 == 0, both at most 2^22, rows at
  * most 2^24, and codes, y and the workspace are 16-byte aligned, scales 4-byte
@@ -74,8 +76,9 @@ polestar_status polestar_mx_linear(int x_fmt, polestar_dtype dtype, long rows, i
 
 /*
  * polestar_mx_quantize_linear -- polestar_mx_quantize of the rows [row_start,
- * row_start + n_rows) of every sequence, then polestar_mx_linear of them, with
- * the same results; the quantized rows stay in the workspace or on chip.
+ * row_start + n_rows) of every sequence, then polestar_mx_linear of them.  The rows
+ * multiplied are the same, bit for bit; the sums may be taken in another order than
+ * polestar_mx_linear's.  The quantized rows stay in the workspace or on chip.
  *   x : [batch][seq][n_in] dtype;  y : out [batch][n_rows][n_out] dtype
  *   workspace : >= polestar_mx_quantize_linear_workspace_size(...) bytes
  * UNSUPPORTED under the conditions of both calls.
@@ -147,7 +150,8 @@ polestar_status polestar_mx_store_kv(polestar_dtype dtype, int batch, int seq, i
  *   workspace : >= polestar_mx_attend_workspace_size(...) bytes (no init)
  * Products are bf16 matrix instructions on the exact key and value numbers;
  * probabilities are rounded to bf16 for bf16 outputs, and for fp32 queries both
- * they and the probabilities are taken as three bf16 terms (24 bits).
+ * they and the probabilities are taken as three bf16 terms (24 bits).  Results of
+ * a magnitude below 2^-126 may be 0.
  * UNSUPPORTED unless head_dim is 64 or 128, n_heads % n_kv_heads == 0 is given
  * (INVALID otherwise), seq <= 2^24, batch and n_kv_heads < 2^16, the query heads'
  * rows fit 2^23 groups of 32 in all, q_stride is a whole number of 16-byte chunks,

@@ -16,13 +16,21 @@
 // barrier: added in pairs with a barrier each, the join took 0.5 to 1.5 us more.
 //
 // Measured inside a graph, head_dim 128, bf16: 8 x 32 heads, 1 query: 256 keys 5.6
-// us, 2048 keys 15.3, 8192 keys 65 (its 285 MB at 4.4 TB/s); 4 x 4 KV heads, 448
-// queries each: 1024 keys 11.3 us, 8192 keys 47.  Long caches of few queries are
-// bound by memory, many queries by the vector unit (187 instructions for the 16
-// matrix instructions of a step, 64 of them the codes' decoding).  Computing the
-// next step's scores beside this step's softmax was 5% slower, twelve waves or two
-// steps of prefetch no faster, nor was an order that keeps a head's query tiles on
-// one XCD.
+// us, 2048 keys 15.3, 8192 keys 54 to 65 (its 285 MB at 4.4 to 5.3 TB/s); 4 x 4 KV
+// heads, 448 queries each: 1024 keys 11.3 us, 8192 keys 47.  Long caches of few queries
+// are bound by memory.  Many queries saturate no unit: of a compute unit's time with
+// two waves per SIMD the vector units are active in 46% (187 instructions for the 16
+// matrix instructions of a step, 64 of them the codes' decoding, which every tile of
+// 32 queries repeats), the matrix units in 21%, and waves wait in 41% of theirs.
+// Computing the next step's scores beside this step's softmax was 5% slower, twelve
+// waves or two steps of prefetch no faster, nor was an order that keeps a head's query
+// tiles on one XCD.
+//
+// bf16 queries: the probabilities are rounded to bf16 for the second product, as in
+// polestar_attend, and their sum is taken before.  The rounding is at most 2^-8 of a
+// probability; outputs of 64 to 32768 keys were 0.0021 to 0.0023 of their norm off the
+// 64-bit result, 0.0017 of that their own rounding.  A second term would double the
+// second product and add 16 vector instructions to a step.
 //
 // fp32 queries: q and p are taken as three bf16 terms each, so that the products
 // with the exact keys and values keep 24 bits.
@@ -85,7 +93,8 @@ __device__ __forceinline__ void split_bf16(const float* v, uint4* o) {
 // V's rows in LDS: 2 HD bytes of a key and 64 more, and within each 64 bytes (the
 // 32 channels that a lane decodes) the 16-byte chunks XORed by v_swizzle(key), so
 // that the lanes whose stores run together, and the eight rows of a transposed
-// read, lie in different banks.  (Without it half of the LDS cycles were conflicts.)
+// read, lie in different banks.  (Conflicts are 31% of the LDS cycles with it and half
+// without.)
 template <int HD> __device__ __forceinline__ int v_swizzle(int key) { return (HD == 128 ? key : key ^ (key >> 2)) & 3; }
 
 // A head's keys or values: buffers that end with the sequence's last key, so that
@@ -385,8 +394,13 @@ __global__ __launch_bounds__(NW * kWave) void mx_attend_merge_kernel(MxAttArgs a
 // Waves per workgroup and key splits: eight waves where the workgroups are at most the
 // compute units and each wave has two steps (the registers allow two waves on each
 // SIMD), and then as many splits as fill the units in one round, while a wave keeps two
-// steps.  One token of two sequences over 32768 keys, 4 KV heads: 405 us without
-// splits, 13.4 with 32 and their join.
+// steps.  In a graph, us: one token of two sequences over 32768 keys, 4 KV heads (8
+// workgroups): 131 unsplit, 24 with 8 splits, 17.4 with 16, 16.4 with 32 (chosen), 19.0
+// with 64.  More splits than one round holds do not pay: 160 workgroups of 4096 keys 22
+// to 24 unsplit (chosen), 34 with 2, 31 with 3; 240 of 4096 keys 28, 36, 40; 256 of 8192
+// keys 54, 61.  What the rule leaves: 160 workgroups of 16384 keys 78 to 89 unsplit, 70
+// with 3 splits (132: 73 to 75, 67), and, since the host does not know the lengths, one
+// sequence of 8192 keys among 512s, 256 workgroups: 37.5 unsplit, 26.6 with 4 splits.
 struct MxAttPlan {
     int tiles, waves, splits;
     size_t part, total;                                  // bytes: O parts, with the sums

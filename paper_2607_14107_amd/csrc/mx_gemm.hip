@@ -9,9 +9,12 @@
 // fp32 outputs of MXFP8 rows are computed on bf16 instructions from the decoded
 // values: the scaled instruction adds eight neighbouring products at a time with
 // about 14 bits below the largest one (measured: 256 * 256 + 2^2 loses the 2^2),
-// 1.5e-5 of the result's norm on normal data, which fp32 would show.  With MXFP4
-// rows the products of a block span less than those bits and the sums are exact
-// to fp32.
+// 1.5e-5 of the result's norm on normal data, which fp32 would show.  (Decoded channels
+// are exact down to bf16's subnormals: those of blocks with scale bytes 0 to 2 are
+// rounded to multiples of 2^-133.)  With MXFP4 rows the products of a block span less
+// than those bits, and sums are as good as fp32 additions: measured over 1024 channels,
+// exact where the rows' and the weights' scales span a factor of 16 each, and within 2.7
+// 2^-24 of the magnitudes' sum where they span 2^40.
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -160,14 +163,17 @@ __device__ __forceinline__ void mx_tile_coords(const MxGemmArgs& g, int blk, int
 // A workgroup's tile: codes and scales by DMA into LDS slots, one barrier per K tile,
 // a wave's blocks on the 16x16x128 scaled instruction (DEC: four 16x16x32 bf16 ones).
 //
-// What bounds it.  The DMA costs by the cache line, whatever is read of it (2 to 3
-// clocks each and a compute unit's 64 bytes per clock at most): K tiles of whole lines
-// and scales of 16 steps at a time took 512 x 12288 x 4096 from 36.3 to 28.3 us (MXFP8,
-// 1.8 PFLOP/s) and 33.1 to 21.3 (MXFP4, 2.4); there the transfers alone take 23 us, the
-// reads and products alone 24; more slots (8 K tiles in flight) gained nothing, nor did
-// two groups of waves with a step each (a third fewer LDS reads).  The large tiles are
-// bound by power: 12288 x 4096 x 24576 takes 0.92 to 0.96 ms (MXFP8, 2.6 PFLOP/s) and
-// 0.62 (MXFP4, 4.0) at 1.7 and 1.85 GHz with the matrix units 65 and 44% busy.
+// What bounds it.  512 x 12288 x 4096 takes 28.3 us (MXFP8, 1.8 PFLOP/s) and 21.3
+// (MXFP4, 2.4); the MXFP8 one's transfers alone take 23, its fragment reads and products
+// alone 24.  The transfers' time goes by the cache lines they touch more than by bytes
+// (3.64e6 requests to L2, about four clocks of a compute unit each): with K tiles of half
+// lines and scales of one K tile at a time, 5.30e6 requests, it was 36.3 and 33.1 us.
+// More slots (8 K tiles in flight) gained nothing, nor did two groups of waves with a
+// step each (a third fewer LDS reads).  12288 x 4096 x 24576 takes 0.89 to 0.95 ms
+// (MXFP8, 2.6 to 2.8 PFLOP/s) and 0.59 to 0.61 (MXFP4, 4.1 to 4.2).  There the clock
+// falls under the load, three calls in a row from 2.3 GHz to 1.75 and 1.6 while the time
+// grows by a fifth and the cycles shrink; of the cycles the matrix units are busy in two
+// thirds (MXFP8) and half (MXFP4), and waves wait in 28% of theirs.
 template <class T, bool BF16>
 __global__ __launch_bounds__(kMxTileThreads) void mx_tile_kernel(MxGemmArgs g) {
     constexpr int FMT = T::FMT, MI = T::MI, NJ = T::NJ, KS = T::KS, BM = T::BM, BN = T::BN, NS = T::NS;
