@@ -847,12 +847,13 @@ bool mx_shape_ok(long rows, int n_out, int n_in) {
 // Rows that the product's kernel quantizes itself: up to 16 (fp32 4), where a wave has
 // one chunk of the rows and a compute unit one workgroup.  One launch less is 2.7 us
 // less on the host (6.9 instead of 9.6 us a call, queued one after another).  In a
-// graph, against two launches, us: 2048 channels and less gain up to a fifth (1024 x
-// 1024, 1 to 16 rows 3.2 to 4.1, 3.7 to 4.4), 4096 x 4096 costs up to a tenth more (bf16
-// MXFP8, 1 row 6.6, 6.3; 16 rows 8.2, 7.7; fp32, 4 rows 7.8, 6.9; 16 rows 11.9, 8.1).
-// Past the limits every workgroup quantizes chunk after chunk of the same rows: 4224 x
-// 256 6.7 (4.9), 8192 x 2048 10.1 (7.5), 65536 x 256 53 (29), and with two output tiles
-// 512 x 8192 6.5 (4.5), 4096 x 12288 14.1 (11.7).
+// graph, against two launches, us: 1024 x 1024, 1 to 16 rows 3.2 to 4.1 (3.7 to 4.4);
+// 2048 channels up to a tenth less; 4096 channels mostly more, bf16 by up to a fifth,
+// fp32 a quarter: 4096 x 4096, MXFP8, bf16, 1 row 6.6 (6.3), 16 rows 8.2 (7.7), fp32, 4
+// rows 7.8 (6.9); 16 of fp32, which are not taken, 11.9 (8.1).  Past the limits every
+// workgroup quantizes chunk after chunk of the same rows: 4224 x 256 6.7 (4.9), 8192 x
+// 2048 10.1 (7.5), 65536 x 256 53 (29); and 512 x 8192 takes 6.5 (4.5), 4096 x 12288
+// 14.1 (11.7).
 bool mx_few_raw(bool bf16, long rows, int n_out, int n_in) {
     return rows <= (bf16 ? 16 : 4) && n_in <= 128 * kFewSteps * kFewWaves && ceil_div(n_out, 16) <= kMxCus;
 }

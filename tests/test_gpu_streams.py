@@ -115,3 +115,35 @@ def test_commit(P):
     need = P.commit_workspace_size(P.BF16, 1, 32, 126464)
     assert need
     _beside_work_in_progress(lambda s: P.suffix_commit(logits, masked, masked, stream=s), [need, 128, 128, 32])
+
+
+def test_microscaled_calls_on_a_forked_stream_in_a_graph(P):
+    """Captured on a stream that joins the captured one, outputs and scratch made by the calls: every replay gives
+    the eager bits, with eager work that allocates and fills between them."""
+    import torch
+    w = P.mx_quantize(P.MXFP4, _normal(512, 4096))
+    x = _normal(80, 4096)
+    caches = [t.view(2, 1, 4096, -1) for i in range(2) for t in P.mx_quantize(P.MXFP4, _normal(8192, 128, seed=i))]
+    q = _normal(2, 3, 5, 128)
+    y = torch.zeros((80, 512), dtype=torch.bfloat16, device="cuda")
+
+    def calls(s):
+        h = P.mx_quantize(P.MXFP8, x, stream=s)
+        P.mx_linear(P.MXFP8, *h, *w, y, stream=s)
+        return [*h, y, P.mx_attend(q, *caches, stream=s)]
+    want = [t.clone() for t in calls(None)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = calls(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        for t in got:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert all(torch.equal(a, b) for a, b in zip(calls(None)[:2], want))
+        torch.full((1 << 24,), i, dtype=torch.uint8, device="cuda")
